@@ -474,6 +474,107 @@ laser_kv_status_t laser_kv_decode_attention(laser_kv_handle_t h, int32_t layer, 
                                             const int64_t q_strides[2], float softmax_scale, float* out,
                                             void* scratch, size_t scratch_bytes, void* stream);
 
+/* ---- paged cache ---------------------------------------------------------------------------------
+ * A cache for decoding whose entries come and go: entries of many sequences of different lengths in one pool of pages, new
+ * tokens appended behind them, entries evicted by the attention weight they have received. It starts empty, from prompts, or from
+ * a layer's compacted cache (laser_kv_cache_view gives K, V and positions that laser_kv_paged_append takes).
+ *
+ * Entry i of sequence b and KV head h is row i % page_size of head h of page page_table[b][i / page_size]. A handle is one
+ * layer's cache; it holds host-side data only, all device memory is the caller's:
+ *   k_pages, v_pages : dev, element (page, h, row, :) at base + page*kv_strides[0] + h*kv_strides[1] + row*kv_strides[2], rows of
+ *                      head_dim contiguous elements of config.dtype; rows must not overlap. Any order of the three
+ *                      strides will do (head by head or token by token within a page).
+ *   weights          : dev fp32 [n_pages][n_kv_heads][page_size], the attention weight that an entry has received; NULL exactly
+ *                      when config.track_weights is 0.
+ *   pos              : dev int32 [n_pages][n_kv_heads][page_size], the entries' token positions.
+ *   page_table       : dev int32 [n_seqs][max_pages]. Only the pages that hold a sequence's entries (and those that an append
+ *                      fills) are looked up; the caller may change the table between calls. Pages that are appended to,
+ *                      evicted from or that accumulate weights belong to one sequence alone; a cache without weights that is only read may share pages
+ *                      between sequences (a common prefix).
+ *   state            : dev int32 [2][n_seqs]: the entries that each sequence holds, then the tokens it has seen, which is the position
+ *                      that its next token gets. The calls below keep it; the caller may set it between calls (0 for a new
+ *                      sequence, a smaller number of entries to take tokens back).
+ *   workspace        : dev, 256-byte aligned, laser_kv_paged_query_sizes bytes, for this handle alone.
+ * What unused slots hold is never interpreted (it may be NaN), and slots that no call is told to write keep it.
+ * Lengths, counts and page numbers lie on the device, so the host does not see them: one out of range is not followed (nothing is
+ * read or written outside the pool), recorded in the handle's status word, and the results of that sequence are
+ * unspecified. laser_kv_paged_poll_status reports it.
+ * Calls of a handle are asynchronous on `stream`, must be issued to one stream or be ordered by the caller, and may be captured
+ * into a graph, which then follows the lengths, table and contents of the replay. They are ordered against other work on the
+ * stream as described at laser_kv_select_block. Errors of these calls: laser_kv_last_error(NULL). */
+typedef struct laser_kv_paged_ctx* laser_kv_paged_handle_t;
+
+enum { LASER_KV_BF16 = 0, LASER_KV_FP16 = 1 };
+
+/* Zero-initialise, then fill. */
+typedef struct {
+  int32_t n_seqs;              /* rows of the table, at most 65535                               */
+  int32_t n_q_heads;           /* H_q                                                            */
+  int32_t n_kv_heads;          /* H_kv; H_q % H_kv == 0. Up to 16 query heads per KV head (8 of head_dim 256) share one reading of
+                                  the cache, more read it several times                        */
+  int32_t head_dim;            /* 64, 128 or 256                                                 */
+  int32_t page_size;           /* entries of a page: a power of two from 8 to 4096               */
+  int32_t n_pages;             /* pages of the pool                                              */
+  int32_t max_pages;           /* pages of a sequence at most (row length of the table)          */
+  int32_t dtype;               /* of keys, values and queries: LASER_KV_BF16 or LASER_KV_FP16    */
+  int32_t track_weights;       /* 1: entries accumulate attention weights, eviction is possible  */
+  int32_t device;              /* CUDA device ordinal                                            */
+} laser_kv_paged_config_t;
+
+laser_kv_status_t laser_kv_paged_query_sizes(const laser_kv_paged_config_t* cfg, size_t* workspace_bytes);
+
+/* Makes the handle's device current, clears the workspace's counters and reads nothing else. CAPACITY for a short workspace. */
+laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* k_pages, void* v_pages,
+                                      const int64_t kv_strides[3], float* weights, int32_t* pos,
+                                      const int32_t* page_table, int32_t* state, void* workspace,
+                                      size_t workspace_bytes, laser_kv_paged_handle_t* out);
+
+/* Puts counts[b] new entries (n_new of every sequence when counts is NULL) behind sequence b's last one: their keys and values, their
+ * weights, their positions. Afterwards the sequence holds, and unless pos is given has seen, that many more.
+ *   K_new, V_new : dev, config.dtype, element (b, h, i, :) at base + b*strides[0] + h*strides[1] + i*strides[2], rows of head_dim
+ *                  contiguous elements; 16-byte aligned, strides multiples of 8 elements; not inside the pool.
+ *   counts       : dev int32 [n_seqs], 0 <= counts[b] <= n_new, or NULL.
+ *   weights      : dev fp32, element (b, h, i) at weights + b*w_strides[0] + h*w_strides[1] + i (the window scores of a prompt, for
+ *                  instance), or NULL: 0. ERR_STATE when the cache keeps none.
+ *   pos          : dev int32, element (b, h, i) at pos + b*pos_strides[0] + h*pos_strides[1] + i, or NULL: counted on from the
+ *                  tokens seen, the same for all heads. With positions given the tokens seen stay as they are (the caller sets them).
+ * A sequence whose table has no room for its new entries gets none of them (CAPACITY in the status word); one entry whose page
+ * number is out of range is left out. */
+laser_kv_status_t laser_kv_paged_append(laser_kv_paged_handle_t h, const void* K_new, const void* V_new,
+                                        const int64_t k_strides[3], const int64_t v_strides[3], int32_t n_new,
+                                        const int32_t* counts, const float* weights, const int64_t w_strides[2],
+                                        const int32_t* pos, const int64_t pos_strides[2], void* stream);
+
+/* Attention of one new token per sequence over the sequence's entries: for query head hq of KV head h = hq / G,
+ *   x_i = <Q[b][hq], K_i> * scale,  lse[b][hq] = log sum_i exp(x_i),  out[b][hq][:] = sum_i exp(x_i - lse) V_i.
+ * A sequence without entries has out 0 and lse -inf. Products and sums in fp32, rounded once to the output's type; sums over
+ * entries are formed in an order that depends on the lengths and the device's SMs alone.
+ *   Q          : dev, config.dtype, element (b, hq, :) at Q + b*q_strides[0] + hq*q_strides[1]; 16-byte aligned, strides multiples of 8.
+ *   softmax_scale : 0 selects 1/sqrt(head_dim).
+ *   accumulate : nonzero: every entry's weight grows by sum over the G heads of exp(x_i - lse). ERR_STATE when the cache keeps none.
+ *   out        : dev [n_seqs][n_q_heads][head_dim], fp32 (out_fp32 nonzero) or config.dtype; 16-byte aligned.
+ *   lse        : dev fp32 [n_seqs][n_q_heads] (natural logarithm), or NULL. */
+laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void* Q, const int64_t q_strides[2],
+                                           float softmax_scale, int32_t accumulate, void* out, int32_t out_fp32,
+                                           float* lse, void* stream);
+
+/* Brings every sequence that holds more than `keep` entries back to `keep`, each KV head by itself: kept are the entries of positions
+ * below `anchors`, those of the last `recent` positions seen (together at most `keep`; should positions repeat, so that more entries
+ * than `keep` are among them, those of lowest index) and, up to `keep`, the ones of the largest accumulated weight; equal weights:
+ * lower index first; NaN counts as -inf, +inf as protected. Entries stay where they are, except that the last kept entry behind `keep` moves
+ * (key, value, weight, position) to the first slot before `keep` that an evicted one leaves, the last but one to the
+ * second, and so on: attention does not depend on the order, positions tell an entry's age. Pages behind the first
+ * ceil(keep / page_size) of a sequence are then free. Tables of more than 786432 entries: ERR_UNSUPPORTED (half of that on a device that
+ * forms no clusters of sixteen). */
+laser_kv_status_t laser_kv_paged_evict(laser_kv_paged_handle_t h, int32_t keep, int32_t anchors, int32_t recent,
+                                       void* stream);
+
+/* Synchronises `stream` and returns the handle's status word: ERR_INVALID_ARG (a page number, length or count was out of range),
+ * ERR_CAPACITY, ERR_TIMEOUT; clears it. Not to be captured. */
+laser_kv_status_t laser_kv_paged_poll_status(laser_kv_paged_handle_t h, void* stream);
+
+void laser_kv_paged_destroy(laser_kv_paged_handle_t h);
+
 #ifdef __cplusplus
 }
 #endif

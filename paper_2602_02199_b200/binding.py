@@ -25,7 +25,10 @@ EXPORTS = [
     "laser_kv_decode_attention", "laser_kv_decode_attention_scratch_bytes", "laser_kv_collision_probability",
     "laser_kv_set_layer_budget", "laser_kv_set_wait_budget", "laser_kv_window_scores_static_status",
     "laser_kv_lookback_close", "laser_kv_select_tail", "laser_kv_get_counters",
+    "laser_kv_paged_query_sizes", "laser_kv_paged_init", "laser_kv_paged_append", "laser_kv_paged_attention",
+    "laser_kv_paged_evict", "laser_kv_paged_poll_status", "laser_kv_paged_destroy",
 ]
+BF16, FP16 = range(2)
 
 
 class Config(C.Structure):
@@ -58,6 +61,12 @@ class Debug(C.Structure):
 class Counters(C.Structure):
     _fields_ = [("select_calls", C.c_int64), ("blocks", C.c_int64), ("tokens", C.c_int64),
                 ("entries_appended", C.c_int64), ("algorithmic_bytes", C.c_int64)]
+
+
+class PagedConfig(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32),
+                ("track_weights", C.c_int32), ("device", C.c_int32)]
 
 
 class LaserKVError(RuntimeError):
@@ -185,6 +194,20 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.laser_kv_decode_attention_scratch_bytes.argtypes = [vp]
     lib.laser_kv_decode_attention.restype = i32
     lib.laser_kv_decode_attention.argtypes = [vp, i32, vp, p(i64), C.c_float, vp, vp, sz, vp]
+    lib.laser_kv_paged_query_sizes.restype = i32
+    lib.laser_kv_paged_query_sizes.argtypes = [p(PagedConfig), p(sz)]
+    lib.laser_kv_paged_init.restype = i32
+    lib.laser_kv_paged_init.argtypes = [p(PagedConfig), vp, vp, p(i64), vp, vp, vp, vp, vp, sz, p(vp)]
+    lib.laser_kv_paged_append.restype = i32
+    lib.laser_kv_paged_append.argtypes = [vp, vp, vp, p(i64), p(i64), i32, vp, vp, p(i64), vp, p(i64), vp]
+    lib.laser_kv_paged_attention.restype = i32
+    lib.laser_kv_paged_attention.argtypes = [vp, vp, p(i64), C.c_float, i32, vp, i32, vp, vp]
+    lib.laser_kv_paged_evict.restype = i32
+    lib.laser_kv_paged_evict.argtypes = [vp, i32, i32, i32, vp]
+    lib.laser_kv_paged_poll_status.restype = i32
+    lib.laser_kv_paged_poll_status.argtypes = [vp, vp]
+    lib.laser_kv_paged_destroy.restype = None
+    lib.laser_kv_paged_destroy.argtypes = [vp]
     _pycall, _lib = _native_calls(lib, build_if_missing), lib
     return lib
 
@@ -546,3 +569,134 @@ def laser_kv_window_scores_static_status(stream=None):
     """Raises LaserKVError if a kernel of an earlier laser_kv_window_scores_static call on the current
     device recorded an error (and clears it); synchronises the stream."""
     _check(load().laser_kv_window_scores_static_status(_stream_ptr(stream)))
+
+
+# ---- paged cache -----------------------------------------------------------------------------------
+def laser_kv_paged_query_sizes(cfg: PagedConfig) -> int:
+    wb = C.c_size_t()
+    _check(load().laser_kv_paged_query_sizes(C.byref(cfg), C.byref(wb)))
+    return wb.value
+
+
+def _need(condition, message):
+    if not condition:
+        raise LaserKVError(ERR_INVALID_ARG, message)
+
+
+class PagedKV:
+    """One layer's paged cache over the caller's tensors: k_pages, v_pages [n_pages][H_kv][page_size][d] (bfloat16 or float16, or
+    int16 for bfloat16's bits; any strides with a contiguous last dim), page_table int32 [n_seqs][max_pages], weights fp32 and pos
+    int32 [n_pages][H_kv][page_size], state int32 [2][n_seqs] (entries held, tokens seen). pos and state are made here when not given;
+    without weights entries accumulate none and none can be evicted."""
+
+    def __init__(self, k_pages, v_pages, page_table, *, n_q_heads, weights=None, pos=None, state=None):
+        import torch
+        self.lib = load()
+        _need(k_pages.dim() == 4 and page_table.dim() == 2, "paged cache: k_pages has 4 dimensions, page_table 2")
+        _need(k_pages.is_cuda, "paged cache: tensors lie on a CUDA device")
+        n_pages, heads, page_size, d = k_pages.shape
+        n_seqs, max_pages = page_table.shape
+        dev = k_pages.device
+        _need(k_pages.dtype in (torch.bfloat16, torch.float16, torch.int16), "paged cache: keys are bfloat16 or float16")
+        if pos is None:
+            pos = torch.full((n_pages, heads, page_size), -1, dtype=torch.int32, device=dev)
+        if state is None:
+            state = torch.zeros((2, n_seqs), dtype=torch.int32, device=dev)
+        _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.stride() == k_pages.stride(),
+              "paged cache: v_pages differs from k_pages in shape, type or strides")
+        _need(d == 1 or k_pages.stride(3) == 1, "paged cache: the last dimension must be contiguous")
+        for name, t, dtype, shape in (("page_table", page_table, torch.int32, (n_seqs, max_pages)),
+                                      ("pos", pos, torch.int32, (n_pages, heads, page_size)),
+                                      ("state", state, torch.int32, (2, n_seqs)),
+                                      ("weights", weights, torch.float32, (n_pages, heads, page_size))):
+            if t is not None:
+                _need(t.dtype == dtype and tuple(t.shape) == shape and t.is_contiguous(),
+                      f"paged cache: {name} must be a contiguous {dtype} tensor of shape {shape}")
+        for t in (v_pages, page_table, pos, state, weights):
+            _need(t is None or t.device == dev, "paged cache: tensors on different devices")
+        self.k_pages, self.v_pages, self.page_table, self.weights, self.pos, self.state = k_pages, v_pages, page_table, weights, pos, state
+        self.lens, self.seen = state[0], state[1]
+        self.cfg = PagedConfig(n_seqs, n_q_heads, heads, d, page_size, n_pages, max_pages,
+                               FP16 if k_pages.dtype == torch.float16 else BF16, 0 if weights is None else 1, dev.index)
+        self.workspace = torch.empty(laser_kv_paged_query_sizes(self.cfg), dtype=torch.uint8, device=dev)
+        h = C.c_void_p()
+        _check(self.lib.laser_kv_paged_init(C.byref(self.cfg), _ptr(k_pages), _ptr(v_pages), (C.c_int64 * 3)(*k_pages.stride()[:3]),
+                                            _ptr(weights), _ptr(pos), _ptr(page_table), _ptr(state), _ptr(self.workspace),
+                                            self.workspace.numel(), C.byref(h)))
+        self.handle = h
+        self._h = h.value                # what the native call path takes; 0 once closed
+        self._device, self._f32 = dev, torch.float32
+        self._types = (torch.float16,) if k_pages.dtype == torch.float16 else (torch.bfloat16, torch.int16)
+        self._q_shape, self._lse_shape, self._new_shape = (n_seqs, n_q_heads, d), (n_seqs, n_q_heads), (n_seqs, heads)
+        self._empty = torch.empty
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.laser_kv_paged_destroy(self.handle)
+            self.handle = None
+            self._h = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _same(self, t, dtypes, shape, name):
+        _need(t.dtype in dtypes and t.shape == shape and t.device == self._device,
+              f"{name}: expected {dtypes[0]} {tuple(shape)} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+    def laser_kv_paged_append(self, K_new, V_new, counts=None, weights=None, pos=None, stream=None):
+        """K_new, V_new: [n_seqs][H_kv][n_new][d] (any strides with a contiguous last dim); counts int32 [n_seqs]; weights fp32 and pos
+        int32 [n_seqs][H_kv][n_new] with contiguous last dims."""
+        _need(K_new.dim() == 4, "paged_append: K_new has 4 dimensions")
+        n_new = K_new.shape[2]
+        shape = self._new_shape + (n_new,)
+        ks, vs = K_new.stride(), V_new.stride()
+        self._same(K_new, self._types, shape + self._q_shape[2:], "paged_append: K_new")
+        self._same(V_new, self._types, shape + self._q_shape[2:], "paged_append: V_new")
+        _need(ks[3] == 1 and vs[3] == 1, "paged_append: the last dimension must be contiguous")
+        ws = ps = (0, 0)
+        if counts is not None:
+            self._same(counts, (self.pos.dtype,), self._q_shape[:1], "paged_append: counts")
+            _need(counts.is_contiguous(), "paged_append: counts must be contiguous")
+        if weights is not None:
+            self._same(weights, (self._f32,), shape, "paged_append: weights")
+            ws = weights.stride()
+            _need(ws[2] == 1 or n_new == 1, "paged_append: the last dimension must be contiguous")
+        if pos is not None:
+            self._same(pos, (self.pos.dtype,), shape, "paged_append: pos")
+            ps = pos.stride()
+            _need(ps[2] == 1 or n_new == 1, "paged_append: the last dimension must be contiguous")
+        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, _ptr(counts), _ptr(weights), ws, _ptr(pos), ps,
+                                 _stream_ptr(stream))
+        if s:
+            _check(s)
+
+    def laser_kv_paged_attention(self, Q, softmax_scale=0.0, accumulate=False, out=None, lse=None, stream=None):
+        """Q: [n_seqs][H_q][d] of the cache's type (contiguous last dim) -> [n_seqs][H_q][d], fp32 or, where `out` says so, the cache's
+        type. `lse`: fp32 [n_seqs][H_q], receives the logarithm of the sum of exponentials."""
+        self._same(Q, self._types, self._q_shape, "paged_attention: Q")
+        qs = Q.stride()
+        _need(qs[2] == 1, "paged_attention: the last dimension must be contiguous")
+        if out is None:
+            out = self._empty(self._q_shape, dtype=self._f32, device=self._device)
+        else:
+            self._same(out, (self._f32,) + self._types, self._q_shape, "paged_attention: out")
+            _need(out.is_contiguous(), "paged_attention: out must be contiguous")
+        if lse is not None:
+            self._same(lse, (self._f32,), self._lse_shape, "paged_attention: lse")
+            _need(lse.is_contiguous(), "paged_attention: lse must be contiguous")
+        s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(),
+                                    1 if out.dtype == self._f32 else 0, _ptr(lse), _stream_ptr(stream))
+        if s:
+            _check(s)
+        return out
+
+    def laser_kv_paged_evict(self, keep, anchors=0, recent=0, stream=None):
+        s = _pycall.paged_evict(self._h, keep, anchors, recent, _stream_ptr(stream))
+        if s:
+            _check(s)
+
+    def laser_kv_paged_poll_status(self, stream=None):
+        _check(self.lib.laser_kv_paged_poll_status(self._h, _stream_ptr(stream)))

@@ -12,6 +12,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <mutex>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -21,6 +22,8 @@
 #include "stream_gemm.cuh"
 #include "query_proj.cuh"
 #include "decode_attn.cuh"
+#include "paged_attn.cuh"
+#include "paged_cache.cuh"
 
 namespace {
 
@@ -1900,3 +1903,5 @@ laser_kv_status_t laser_kv_gather_append(const void* K_src, const void* V_src, i
 }
 
 }  // extern "C"
+
+#include "paged_host.cuh"

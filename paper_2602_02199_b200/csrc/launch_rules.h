@@ -125,4 +125,22 @@ LKV_HOST_DEVICE inline long long weighted_begin(long long part, int c, int n, co
   return part * w / ((long long)early * s.w_early + (long long)(n - early) * s.w_late);
 }
 
+// Paged cache. The tiles of all sequences and heads are one list that is cut into equal contiguous shares, one per CTA (or
+// warp): share c of n is [paged_share_begin(c), paged_share_begin(c + 1)); with n <= total none is empty.
+LKV_HOST_DEVICE inline int paged_share_begin(int total, int n, int c) { return (int)((long long)total * c / n); }
+// The share that holds tile t.
+LKV_HOST_DEVICE inline int paged_share_owner(int total, int n, int t) { return (int)((((long long)t + 1) * n - 1) / total); }
+// Shares of an attention call on `grid` CTAs.
+LKV_HOST_DEVICE inline int paged_shares(int total, int grid) { return total < grid ? total : grid; }
+
+// CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: as many as fill the SMs once, of a thousand
+// entries at least, of at most kEvictKeys (their sort keys stay in shared memory). 0: more entries than `most` CTAs hold.
+constexpr int kEvictKeys = 49152;
+inline int evict_cluster(int num_sms, long long heads, long long cap, int most) {
+  int n = 1;
+  while (n < most && 2 * n * heads <= num_sms && cap > 1024ll * n) n *= 2;
+  while (n < most && cap > (long long)kEvictKeys * n) n *= 2;
+  return cap > (long long)kEvictKeys * n ? 0 : n;
+}
+
 }  // namespace lkv

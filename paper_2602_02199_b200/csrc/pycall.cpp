@@ -19,6 +19,9 @@ decltype(&laser_kv_gather_append) f_gather_append;
 decltype(&laser_kv_window_scores) f_window_scores;
 decltype(&laser_kv_collision_counts) f_collision_counts;
 decltype(&laser_kv_consensus_accumulate) f_consensus_accumulate;
+decltype(&laser_kv_paged_append) f_paged_append;
+decltype(&laser_kv_paged_attention) f_paged_attention;
+decltype(&laser_kv_paged_evict) f_paged_evict;
 
 // The arguments of one call, taken in order; a failed conversion leaves a Python error.
 struct Args {
@@ -180,6 +183,49 @@ PyObject* py_consensus_accumulate(PyObject*, PyObject* const* argv, Py_ssize_t n
   return call(a, [&] { return f_consensus_accumulate(s, c, batch, heads, nb, S, carry, sa, ca, stream); });
 }
 
+PyObject* py_paged_append(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  if (!count_is(n, 12)) return nullptr;
+  Args a{argv};
+  auto h = static_cast<laser_kv_paged_handle_t>(a.ptr());
+  void *k = a.ptr(), *v = a.ptr();
+  int64_t ks[3] = {0, 0, 0}, vs[3] = {0, 0, 0}, ws[2] = {0, 0}, ps[2] = {0, 0};
+  a.strides(ks);
+  a.strides(vs);
+  const int32_t n_new = a.i32();
+  auto counts = static_cast<const int32_t*>(a.ptr());
+  auto w = static_cast<const float*>(a.ptr());
+  a.strides(ws);
+  auto pos = static_cast<const int32_t*>(a.ptr());
+  a.strides(ps);
+  void* stream = a.ptr();
+  return call(a, [&] { return f_paged_append(h, k, v, ks, vs, n_new, counts, w, ws, pos, ps, stream); });
+}
+
+PyObject* py_paged_attention(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  if (!count_is(n, 9)) return nullptr;
+  Args a{argv};
+  auto h = static_cast<laser_kv_paged_handle_t>(a.ptr());
+  void* q = a.ptr();
+  int64_t qs[2] = {0, 0};
+  a.strides(qs);
+  const float scale = a.f32();
+  const int32_t accumulate = a.i32();
+  void* out = a.ptr();
+  const int32_t fp32 = a.i32();
+  float* lse = static_cast<float*>(a.ptr());
+  void* stream = a.ptr();
+  return call(a, [&] { return f_paged_attention(h, q, qs, scale, accumulate, out, fp32, lse, stream); });
+}
+
+PyObject* py_paged_evict(PyObject*, PyObject* const* argv, Py_ssize_t n) {
+  if (!count_is(n, 5)) return nullptr;
+  Args a{argv};
+  auto h = static_cast<laser_kv_paged_handle_t>(a.ptr());
+  const int32_t keep = a.i32(), anchors = a.i32(), recent = a.i32();
+  void* stream = a.ptr();
+  return call(a, [&] { return f_paged_evict(h, keep, anchors, recent, stream); });
+}
+
 template <typename F>
 bool resolve(void* lib, const char* name, F& f) {
   f = reinterpret_cast<F>(dlsym(lib, name));
@@ -198,7 +244,8 @@ PyObject* py_setup(PyObject*, PyObject* path) {
       !resolve(lib, "laser_kv_decode_attention", f_decode_attention) || !resolve(lib, "laser_kv_two_stage_topk", f_two_stage_topk) ||
       !resolve(lib, "laser_kv_gather_append", f_gather_append) || !resolve(lib, "laser_kv_window_scores", f_window_scores) ||
       !resolve(lib, "laser_kv_collision_counts", f_collision_counts) ||
-      !resolve(lib, "laser_kv_consensus_accumulate", f_consensus_accumulate))
+      !resolve(lib, "laser_kv_consensus_accumulate", f_consensus_accumulate) || !resolve(lib, "laser_kv_paged_append", f_paged_append) ||
+      !resolve(lib, "laser_kv_paged_attention", f_paged_attention) || !resolve(lib, "laser_kv_paged_evict", f_paged_evict))
     return nullptr;
   Py_RETURN_NONE;
 }
@@ -213,6 +260,9 @@ PyMethodDef methods[] = {{"setup", py_setup, METH_O, nullptr},
                          LKV_FAST(window_scores),
                          LKV_FAST(collision_counts),
                          LKV_FAST(consensus_accumulate),
+                         LKV_FAST(paged_append),
+                         LKV_FAST(paged_attention),
+                         LKV_FAST(paged_evict),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pycall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
