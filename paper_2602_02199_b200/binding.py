@@ -625,9 +625,10 @@ class PagedKV:
                                             self.workspace.numel(), C.byref(h)))
         self.handle = h
         self._h = h.value                # what the native call path takes; 0 once closed
-        self._device, self._f32 = dev, torch.float32
+        self._device, self._f32, self._i32 = dev, torch.float32, torch.int32
         self._types = (torch.float16,) if k_pages.dtype == torch.float16 else (torch.bfloat16, torch.int16)
-        self._q_shape, self._lse_shape, self._new_shape = (n_seqs, n_q_heads, d), (n_seqs, n_q_heads), (n_seqs, heads)
+        self._q_shape, self._lse_shape = (n_seqs, n_q_heads, d), (n_seqs, n_q_heads)
+        self._n_seqs, self._heads, self._d = n_seqs, heads, d
         self._empty = torch.empty
 
     def close(self):
@@ -642,53 +643,60 @@ class PagedKV:
         except Exception:
             pass
 
-    def _same(self, t, dtypes, shape, name):
-        _need(t.dtype in dtypes and t.shape == shape and t.device == self._device,
-              f"{name}: expected {dtypes[0]} {tuple(shape)} on {self._device}, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    def _refuse(self, t, dtypes, shape, name):
+        raise LaserKVError(ERR_INVALID_ARG, f"{name}: expected {' or '.join(str(x) for x in dtypes)} {tuple(shape)} with a contiguous last "
+                           f"dimension on {self._device}, got {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}")
 
     def laser_kv_paged_append(self, K_new, V_new, counts=None, weights=None, pos=None, stream=None):
         """K_new, V_new: [n_seqs][H_kv][n_new][d] (any strides with a contiguous last dim); counts int32 [n_seqs]; weights fp32 and pos
         int32 [n_seqs][H_kv][n_new] with contiguous last dims."""
-        _need(K_new.dim() == 4, "paged_append: K_new has 4 dimensions")
-        n_new = K_new.shape[2]
-        shape = self._new_shape + (n_new,)
-        ks, vs = K_new.stride(), V_new.stride()
-        self._same(K_new, self._types, shape + self._q_shape[2:], "paged_append: K_new")
-        self._same(V_new, self._types, shape + self._q_shape[2:], "paged_append: V_new")
-        _need(ks[3] == 1 and vs[3] == 1, "paged_append: the last dimension must be contiguous")
+        n_seqs, heads, d, dev, i32 = self._n_seqs, self._heads, self._d, self._device, self._i32
+        kshape, ks, vs = K_new.shape, K_new.stride(), V_new.stride()
+        n_new = kshape[2] if len(kshape) == 4 else -1
+        if kshape != (n_seqs, heads, n_new, d) or ks[3] != 1 or K_new.dtype not in self._types or K_new.device != dev:
+            self._refuse(K_new, self._types, (n_seqs, heads, n_new, d), "paged_append: K_new")
+        if V_new.shape != kshape or vs[3] != 1 or V_new.dtype not in self._types or V_new.device != dev:
+            self._refuse(V_new, self._types, kshape, "paged_append: V_new")
+        c = w = at = 0
         ws = ps = (0, 0)
         if counts is not None:
-            self._same(counts, (self.pos.dtype,), self._q_shape[:1], "paged_append: counts")
-            _need(counts.is_contiguous(), "paged_append: counts must be contiguous")
+            if counts.shape != (n_seqs,) or counts.dtype != i32 or counts.device != dev or not counts.is_contiguous():
+                self._refuse(counts, (i32,), (n_seqs,), "paged_append: counts")
+            c = counts.data_ptr()
         if weights is not None:
-            self._same(weights, (self._f32,), shape, "paged_append: weights")
             ws = weights.stride()
-            _need(ws[2] == 1 or n_new == 1, "paged_append: the last dimension must be contiguous")
+            if weights.shape != (n_seqs, heads, n_new) or weights.dtype != self._f32 or weights.device != dev or (n_new > 1 and ws[2] != 1):
+                self._refuse(weights, (self._f32,), (n_seqs, heads, n_new), "paged_append: weights")
+            w = weights.data_ptr()
         if pos is not None:
-            self._same(pos, (self.pos.dtype,), shape, "paged_append: pos")
             ps = pos.stride()
-            _need(ps[2] == 1 or n_new == 1, "paged_append: the last dimension must be contiguous")
-        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, _ptr(counts), _ptr(weights), ws, _ptr(pos), ps,
-                                 _stream_ptr(stream))
+            if pos.shape != (n_seqs, heads, n_new) or pos.dtype != i32 or pos.device != dev or (n_new > 1 and ps[2] != 1):
+                self._refuse(pos, (i32,), (n_seqs, heads, n_new), "paged_append: pos")
+            at = pos.data_ptr()
+        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, c, w, ws, at, ps, _stream_ptr(stream))
         if s:
             _check(s)
 
     def laser_kv_paged_attention(self, Q, softmax_scale=0.0, accumulate=False, out=None, lse=None, stream=None):
         """Q: [n_seqs][H_q][d] of the cache's type (contiguous last dim) -> [n_seqs][H_q][d], fp32 or, where `out` says so, the cache's
         type. `lse`: fp32 [n_seqs][H_q], receives the logarithm of the sum of exponentials."""
-        self._same(Q, self._types, self._q_shape, "paged_attention: Q")
-        qs = Q.stride()
-        _need(qs[2] == 1, "paged_attention: the last dimension must be contiguous")
+        shape, dev, qs, f32 = self._q_shape, self._device, Q.stride(), self._f32
+        if Q.shape != shape or qs[2] != 1 or Q.dtype not in self._types or Q.device != dev:
+            self._refuse(Q, self._types, shape, "paged_attention: Q")
+        is32 = 1
         if out is None:
-            out = self._empty(self._q_shape, dtype=self._f32, device=self._device)
+            out = self._empty(shape, dtype=f32, device=dev)
         else:
-            self._same(out, (self._f32,) + self._types, self._q_shape, "paged_attention: out")
-            _need(out.is_contiguous(), "paged_attention: out must be contiguous")
+            is32 = out.dtype == f32
+            if out.shape != shape or not out.is_contiguous() or not (is32 or out.dtype in self._types) or out.device != dev:
+                self._refuse(out, (f32,) + self._types, shape, "paged_attention: contiguous out")
+        z = 0
         if lse is not None:
-            self._same(lse, (self._f32,), self._lse_shape, "paged_attention: lse")
-            _need(lse.is_contiguous(), "paged_attention: lse must be contiguous")
-        s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(),
-                                    1 if out.dtype == self._f32 else 0, _ptr(lse), _stream_ptr(stream))
+            if lse.shape != self._lse_shape or not lse.is_contiguous() or lse.dtype != f32 or lse.device != dev:
+                self._refuse(lse, (f32,), self._lse_shape, "paged_attention: contiguous lse")
+            z = lse.data_ptr()
+        s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(), is32, z,
+                                    _stream_ptr(stream))
         if s:
             _check(s)
         return out

@@ -125,13 +125,18 @@ LKV_HOST_DEVICE inline long long weighted_begin(long long part, int c, int n, co
   return part * w / ((long long)early * s.w_early + (long long)(n - early) * s.w_late);
 }
 
-// Paged cache. The tiles of all sequences and heads are one list that is cut into equal contiguous shares, one per CTA (or
-// warp): share c of n is [paged_share_begin(c), paged_share_begin(c + 1)); with n <= total none is empty.
+// Paged cache. The items (a sequence and a KV head) are one list of units, kPagedItemUnits for each item and one for each of its
+// tiles, that is cut into equal contiguous shares, one per CTA (or warp): share c of n is [paged_share_begin(c),
+// paged_share_begin(c + 1)); with n <= total none is empty.
+constexpr int kPagedItemUnits = 2;
 LKV_HOST_DEVICE inline int paged_share_begin(int total, int n, int c) { return (int)((long long)total * c / n); }
-// The share that holds tile t.
+// The share that holds unit t.
 LKV_HOST_DEVICE inline int paged_share_owner(int total, int n, int t) { return (int)((((long long)t + 1) * n - 1) / total); }
-// Shares of an attention call on `grid` CTAs.
-LKV_HOST_DEVICE inline int paged_shares(int total, int grid) { return total < grid ? total : grid; }
+// Shares of an attention call on `grid` CTAs: of two units at least.
+LKV_HOST_DEVICE inline int paged_shares(int total, int grid) {
+  const int n = total - total / 2;
+  return n < grid ? n : grid;
+}
 
 // CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: as many as fill the SMs once, of a thousand
 // entries at least, of at most kEvictKeys (their sort keys stay in shared memory). 0: more entries than `most` CTAs hold.

@@ -60,26 +60,28 @@ struct PagedAttnArgs {
   float* lse2;                                             // the same in log2 units, for paged_weights_kernel; NULL without
   float* scores;                                           // [tile of all heads][64][Gs]; NULL without weights
   float* weights;                                          // [n_pages][H][page_size]
-  int score_tiles;                                         // tiles that `scores` holds
-  float* part;                                             // [CTA][2] partials
+  int2* score_at;                                          // [units of all heads] sequence and KV head of a tile of `scores`, tile of the sequence
+  int* score_units;                                        // units in use
+  int score_tiles;                                         // units that `scores` and `score_at` hold
+  float* part;                                             // [2][grid] partials
   int* tickets;                                            // [n_seqs][H][head blocks] parts that are done; zero between calls
-  int G, Gs, head_blocks;                                  // query heads per KV head, rounded up to even; blocks of NG * 8 of them
+  int G, Gs, head_blocks;                                  // query heads per KV head, up to a power of two from 4 on; blocks of NG * 8 of them
   int out16;
   float scale_log2e;
 };
 
 template <int D>
 __host__ __device__ constexpr int paged_stage_bytes() { return kDecTile * D * 4; }
-// Stages: 96 KB of tiles in flight per CTA, two CTAs per SM; heads of 256 have 192 KB and the SM to themselves.
+// 192 KB of tiles in flight per SM, of three, two or one CTAs.
 template <int D>
-__host__ __device__ constexpr int paged_stages() { return D == 64 ? 6 : 3; }
+__host__ __device__ constexpr int paged_stages() { return D == 64 ? 4 : 3; }
 template <int D>
-__host__ __device__ constexpr int paged_ctas_per_sm() { return D == 256 ? 1 : 2; }
+__host__ __device__ constexpr int paged_ctas_per_sm() { return D == 64 ? 3 : 256 / D; }
 template <int D, int NG>
 __host__ __device__ constexpr int paged_part_floats() { return NG * 8 * (D + 2); }
 template <int D, int NG>
 __host__ __device__ constexpr uint32_t paged_smem_bytes() {
-  return 1024u + paged_stages<D>() * paged_stage_bytes<D>() + 2u * D / 16 * 512u + 2u * kPagedWarps * NG * 8u * 4u + 2u * paged_stages<D>() * 8u + 16u;
+  return 1024u + paged_stages<D>() * paged_stage_bytes<D>() + 2u * D / 16 * 512u + 2u * kPagedWarps * NG * 8u * 4u + (2u * paged_stages<D>() + 2u) * 8u + 16u;
 }
 
 // D (16x8, fp32) += A (16x16, row) * B (16x8, col)
@@ -109,29 +111,40 @@ __device__ __forceinline__ float2 paged_unpack(uint32_t x) {
 }
 __device__ __forceinline__ void paged_consumers_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kPagedWarps * 32) : "memory"); }
 
-// Where a warp is in the list of tiles: sequences one after the other, in each `heads` items, in each the sequence's tiles.
+// Where a warp is in the list: sequences one after the other, in each `heads` items, in each kPagedItemUnits units for the
+// item itself and one for each of the sequence's tiles.
 struct PagedWalk {
-  int b, head, tile, n_tiles;                              // sequence, item in it, tile of the item, the sequence's tiles per item
-  int len;
-  int before;                                              // tiles per item of the sequences before this one
-  __device__ __forceinline__ void next_item(const PagedPool& p, int heads) {
-    tile = 0;
-    if (++head < heads) return;
+  int b, head;                                             // sequence, item in it
+  int len, n_tiles;                                        // of the sequence
+  int before;                                              // units per item of the sequences before this one
+  int unit0;                                               // the item's first unit
+  __device__ __forceinline__ int units() const { return n_tiles + kPagedItemUnits; }
+  // The item's tiles in the units [begin, stop) are [first, last); none where first >= last.
+  __device__ __forceinline__ int first(int begin) const { return max(0, begin - unit0 - kPagedItemUnits); }
+  __device__ __forceinline__ int last(int stop) const { return min(n_tiles, stop - unit0 - kPagedItemUnits); }
+  // The next item starts before `stop`, or there is none to go on with.
+  __device__ __forceinline__ bool next(const PagedPool& p, int heads, int stop) {
+    unit0 += units();
+    if (unit0 >= stop) return false;
+    if (++head < heads) return true;
     head = 0;
+    before += units();
     do {
-      before += n_tiles;
       ++b;
-      len = b < p.n_seqs ? p.length(b) : 1;                // past the end: not asked for any more
+      len = p.length(b);                                   // the list goes on: there is a sequence with entries
       n_tiles = (len + kDecTile - 1) / kDecTile;
     } while (n_tiles == 0);
+    return true;
   }
 };
 
-// Tiles per item over all sequences; called by whole warps. `mine`: this lane's part, see paged_seek.
+__device__ __forceinline__ int paged_units(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile + kPagedItemUnits : 0; }
+
+// Units per item over all sequences; called by whole warps. `mine`: this lane's part, see paged_seek.
 __device__ __forceinline__ int paged_total(const PagedPool& p, int lane, int& mine) {
   const int per = (p.n_seqs + 31) / 32;
   mine = 0;
-  for (int i = lane * per; i < min((lane + 1) * per, p.n_seqs); ++i) mine += (p.length(i) + kDecTile - 1) / kDecTile;
+  for (int i = lane * per; i < min((lane + 1) * per, p.n_seqs); ++i) mine += paged_units(p.length(i));
   return __reduce_add_sync(0xffffffffu, mine);
 }
 __device__ __forceinline__ int warp_inclusive(int x, int lane) {
@@ -142,38 +155,54 @@ __device__ __forceinline__ int warp_inclusive(int x, int lane) {
   }
   return x;
 }
-// The place of tile `at` (below total * heads) of the list.
+// The place of unit `at` (below total * heads) of the list.
 __device__ __forceinline__ PagedWalk paged_seek(const PagedPool& p, int lane, int mine, int heads, int at) {
-  const int per = (p.n_seqs + 31) / 32, q = at / heads;    // the sequence: the first with more than q tiles per item up to its end
+  const int per = (p.n_seqs + 31) / 32, q = at / heads;    // the sequence: the first with more than q units per item up to its end
   int incl = warp_inclusive(mine, lane);
-  const int who = __ffs(__ballot_sync(0xffffffffu, incl > q)) - 1;
+  const int who = (__ffs(__ballot_sync(0xffffffffu, incl > q)) - 1) & 31;
   PagedWalk w;
   w.before = __shfl_sync(0xffffffffu, incl - mine, who);
   w.b = who * per;
   for (;;) {
     const int i = w.b + lane;
-    const int len = i < p.n_seqs ? p.length(i) : 0, t = (len + kDecTile - 1) / kDecTile;
-    incl = w.before + warp_inclusive(t, lane);
+    const int len = i < p.n_seqs ? p.length(i) : 0, u = paged_units(len);
+    incl = w.before + warp_inclusive(u, lane);
     const uint32_t found = __ballot_sync(0xffffffffu, incl > q);
-    const int l = found ? __ffs(found) - 1 : 31;
-    if (found) {
+    if (found || w.b + 32 >= p.n_seqs) {                   // `at` is in the list: found
+      const int l = (__ffs(found) - 1) & 31;
       w.b += l;
-      w.before = __shfl_sync(0xffffffffu, incl - t, l);
-      w.len = __shfl_sync(0xffffffffu, len, l);
-      w.n_tiles = __shfl_sync(0xffffffffu, t, l);
+      w.before = __shfl_sync(0xffffffffu, incl - u, l);
+      w.len = max(1, __shfl_sync(0xffffffffu, len, l));
       break;
     }
     w.before = __shfl_sync(0xffffffffu, incl, 31);
     w.b += 32;
-    if (w.b >= p.n_seqs) {                                 // cannot be: `at` is in the list
-      w.len = w.n_tiles = 1;
-      break;
-    }
   }
-  const int r = at - w.before * heads;
-  w.head = r / w.n_tiles;
-  w.tile = r - w.head * w.n_tiles;
+  w.n_tiles = (w.len + kDecTile - 1) / kDecTile;
+  w.head = (at - w.before * heads) / w.units();
+  w.unit0 = w.before * heads + w.head * w.units();
   return w;
+}
+
+// TMA load of what is read once: its lines leave the L2 cache before the others, scores and old weights among them.
+__device__ __forceinline__ uint64_t l2_evict_first() {
+  uint64_t policy;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+__device__ __forceinline__ void tma_load_4d_once(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2, int c3,
+                                                 uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(dst),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy)
+      : "memory");
+}
+__device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+__device__ __forceinline__ int atom_add_acq_rel(int* p, int v) {
+  int old;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(old) : "l"(p), "r"(v) : "memory");
+  return old;
 }
 
 template <bool HALF, int D, int NG>
@@ -191,16 +220,25 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   const uint32_t bars = smem_u32(s_last) + 16u;
   auto bar_full = [&](int s) { return bars + 8u * s; };
   auto bar_empty = [&](int s) { return bars + 8u * (kStages + s); };
+  auto bar_join = [&](int s) { return bars + 8u * (2 * kStages + s); };
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PagedPool& p = a.pool;
   const int heads = p.H * a.head_blocks;
 
   if (tid == kPagedWarps * 32) {
     for (int s = 0; s < kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), kPagedWarps); }
+    for (int s = 0; s < 2; ++s) mbar_init(bar_join(s), 1);
     fence_mbar_init();
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
   }
+  // Lengths, page numbers and queries are asked for one after the other: the L2 cache gets them together and ahead.
+  {
+    const long long at = ((long long)blockIdx.x * kPagedThreads + tid) * 128, table = (long long)p.n_seqs * p.max_pages * 4;
+    if (at < table) prefetch_l2(reinterpret_cast<const char*>(p.table) + at);
+    if (at < p.n_seqs * 4) prefetch_l2(reinterpret_cast<const char*>(p.lens) + at);
+  }
+  __syncthreads();                                                 // the barriers are set up
   // launched beside the kernel ahead in the stream: nothing is read or written before that is complete
   grid_dependency_wait();
   allow_dependents();
@@ -210,22 +248,24 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   const int n_act = paged_shares(total, (int)gridDim.x);
   const int cta = blockIdx.x;
   const int begin = cta < n_act ? paged_share_begin(total, n_act, cta) : 0;
-  int left = cta < n_act ? paged_share_begin(total, n_act, cta + 1) - begin : 0;
+  const int stop = cta < n_act ? paged_share_begin(total, n_act, cta + 1) : 0;
+  bool more = begin < stop;
   PagedWalk w{};
-  if (left > 0) w = paged_seek(p, lane, mine, heads, begin);
-  __syncthreads();                                                 // the barriers are set up
+  if (more) w = paged_seek(p, lane, mine, heads, begin);
+  if (a.scores && cta == 0 && tid == 0) *a.score_units = total / a.head_blocks;
 
   if (warp == kPagedWarps) {
     // ---- producer ---------------------------------------------------------------------------------
     const int rows_shift = min(p.page_shift, 6);                   // rows of a box
     const int per_shift = 6 - rows_shift;                          // pages of a tile
+    const uint64_t once = l2_evict_first();
     int st = 0, round = 0;
-    while (left > 0) {
-      const int n = min(left, w.n_tiles - w.tile), end = w.tile + n, h = w.head / a.head_blocks;
+    for (; more; more = w.next(p, heads, stop)) {
+      const int first = w.first(begin), end = w.last(stop), h = w.head / a.head_blocks;
       const int last_page = (w.len - 1) >> p.page_shift;
       int ids = 0;
-      for (int t = w.tile; t < end; ++t) {
-        const int chunk = 32 >> per_shift, k = (t - w.tile) & (chunk - 1);   // tiles whose page numbers the lanes hold
+      for (int t = first; t < end; ++t) {
+        const int chunk = 32 >> per_shift, k = (t - first) & (chunk - 1);   // tiles whose page numbers the lanes hold
         if (k == 0) {
           const int at = per_shift ? (t << per_shift) + lane : ((t + lane) << 6) >> p.page_shift;
           ids = at <= last_page ? p.table[(long long)w.b * p.max_pages + at] : 0;
@@ -238,24 +278,27 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         const int id = __shfl_sync(0xffffffffu, ids, (k << per_shift) + (lane & ((1 << per_shift) - 1)));
         if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_empty(st), (uint32_t)(round - 1) & 1u))) {
           if (lane == 0) record_status(p.status, kStatusTimeout);
-          left = n;                                                // the consumers give up, too
-          break;
+          return;                                                  // the consumers' waits run out, too
         }
         if (lane == 0) mbar_expect_tx(bar_full(st), (uint32_t)pages << (rows_shift + 7 + (D == 64 ? 1 : D == 128 ? 2 : 3)));
         __syncwarp();
+        if (a.scores) {                                            // for paged_weights_kernel: the old weights, eight to a sector
+          const int e = (lane & 7) << 3, pg = per_shift ? e >> rows_shift : 0;
+          const int wid = __shfl_sync(0xffffffffu, ids, (k << per_shift) + pg);
+          if (lane < 8 && e < rows && wid < p.n_pages)
+            prefetch_l2(a.weights + (((long long)wid * p.H + h) << p.page_shift) + (((t << 6) + e) & (p.page_size() - 1)));
+        }
         if (lane < pages) {
           const uint32_t dst = base + st * paged_stage_bytes<D>() + ((uint32_t)lane << (rows_shift + 7));
           const int row = per_shift ? 0 : (t << 6) & (p.page_size() - 1);
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + c * kBox, &map_k, bar_full(st), 64 * c, row, h, id);
+          for (int c = 0; c < D / 64; ++c) tma_load_4d_once(dst + c * kBox, &map_k, bar_full(st), 64 * c, row, h, id, once);
 #pragma unroll
-          for (int c = 0; c < D / 64; ++c) tma_load_4d(dst + kHalf + c * kBox, &map_v, bar_full(st), 64 * c, row, h, id);
+          for (int c = 0; c < D / 64; ++c) tma_load_4d_once(dst + kHalf + c * kBox, &map_v, bar_full(st), 64 * c, row, h, id, once);
         }
         __syncwarp();
         if (++st == kStages) { st = 0; ++round; }
       }
-      left -= n;
-      if (left > 0) w.next_item(p, heads);
     }
     return;
   }
@@ -376,11 +419,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     }
   };
 
-  int st = 0, round = 0;
-  bool gone = false;                                               // a wait ran out: the list is walked, nothing is computed
-  while (left > 0) {
-    const int n = min(left, w.n_tiles - w.tile), h = w.head / a.head_blocks, first = (w.head - h * a.head_blocks) * NG * 8;
-    uint32_t qb[NG][MT][2];                                        // B fragments of Q^T, heads past G are zero
+  uint32_t qb[NG][MT][2];                                          // B fragments of Q^T, heads past G are zero
+  auto load_q = [&]() {
+    const int h = w.head / a.head_blocks, first = (w.head - h * a.head_blocks) * NG * 8;
 #pragma unroll
     for (int ng = 0; ng < NG; ++ng) {
       const int hg = first + ng * 8 + g;
@@ -391,9 +432,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         qb[ng][ks][1] = hg < a.G ? *reinterpret_cast<const uint32_t*>(q + 16 * ks + 8 + 2 * c) : 0u;
       }
     }
+  };
+  constexpr bool kAhead = NG == 1;                                 // two sets' queries take too many registers during a merge
+  if (kAhead && more) load_q();
+  int st = 0, round = 0;
+  bool gone = false;                                               // a wait ran out: the list is walked, nothing is computed
+  while (more) {
+    const int t0 = w.first(begin), t1 = w.last(stop);
+    if (t0 >= t1) break;                                           // the share ends with units of the item itself
+    const int h = w.head / a.head_blocks, first = (w.head - h * a.head_blocks) * NG * 8;
+    if (!kAhead) load_q();
     clear();
-    const int score_tile = w.before * p.H + h * w.n_tiles;
-    for (int t = w.tile; t < w.tile + n; ++t) {
+    const int score_unit = w.before * p.H + h * w.units();           // of the item
+    if (a.scores && tid < (t0 == 0 ? kPagedItemUnits : 0) && score_unit + tid < a.score_tiles) a.score_at[score_unit + tid] = make_int2(0, -1);
+    for (int t = t0; t < t1; ++t) {
       if (!gone && !__all_sync(0xffffffffu, mbar_wait(bar_full(st), (uint32_t)round & 1u))) {
         if (lane == 0) record_status(p.status, kStatusTimeout);
         gone = true;
@@ -414,7 +466,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
 #pragma unroll
           for (int ng = 0; ng < NG; ++ng) {
             paged_mma<HALF>(s[ng], k0, qb[ng][ks][0], qb[ng][ks][1]);
-            paged_mma<HALF>(s1[ng], k1, qb[ng][ks + 1][0], qb[ng][ks + 1][1]);
+            paged_mma<HALF>(NG == 1 ? s1[ng] : s[ng], k1, qb[ng][ks + 1][0], qb[ng][ks + 1][1]);   // two chains in all
           }
         }
         // rows past the sequence's end hold whatever the page or an earlier tile left there
@@ -427,10 +479,12 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         for (int ng = 0; ng < NG; ++ng) {
           float x[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v_lo : v_hi) ? (s[ng][i] + s1[ng][i]) * a.scale_log2e : -INFINITY;
-          if (a.scores && score_tile + t < a.score_tiles) {
+          for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v_lo : v_hi) ? (NG == 1 ? s[ng][i] + s1[ng][i] : s[ng][i]) * a.scale_log2e : -INFINITY;
+          const int unit = score_unit + kPagedItemUnits + t;
+          if (a.scores && unit < a.score_tiles) {
             const int hg = first + ng * 8 + 2 * c;
-            float* dst = a.scores + ((long long)(score_tile + t) * kDecTile + warp * 16 + g) * a.Gs + hg;
+            if (ng == 0 && tid == 0) a.score_at[unit] = make_int2((int)((unsigned)w.b | (unsigned)h << 16), t);
+            float* dst = a.scores + ((long long)unit * kDecTile + warp * 16 + g) * a.Gs + hg;
             if (hg < a.G) {
               if (v_lo) *reinterpret_cast<float2*>(dst) = make_float2(x[0], x[1]);
               if (v_hi) *reinterpret_cast<float2*>(dst + 8 * a.Gs) = make_float2(x[2], x[3]);
@@ -503,121 +557,177 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int off = 4; off < 32; off <<= 1) l[ng][x] += __shfl_xor_sync(0xffffffffu, l[ng][x], off);
+    // the next item's queries are on their way while this one's results are merged
+    const int b = w.b, head = w.head, item = b * heads + head, n_tiles = w.n_tiles, unit0 = w.unit0;
+    more = w.next(p, heads, stop) && w.last(stop) > 0;             // not just units of the next item itself
+    if (kAhead && more) load_q();
     merge_warps();
-    const bool whole = n == w.n_tiles;
-    if (whole) {
-      if (warp == 0) finish(w.b, w.head);
-    } else {
-      // the item's parts lie in consecutive CTAs: its start in the first one's second slot, the others in their first
-      constexpr int kPart = paged_part_floats<D, NG>();
-      const int t0 = (w.before * heads) + w.head * w.n_tiles, item = w.b * heads + w.head;
-      const int from = paged_share_owner(total, n_act, t0), to = paged_share_owner(total, n_act, t0 + w.n_tiles - 1);
-      if (warp == 0) {
-        float* dst = a.part + ((long long)cta * 2 + (w.tile == 0 ? 1 : 0)) * kPart;
+    if (t1 - t0 == n_tiles) {
+      if (warp == 0) finish(b, head);
+      continue;
+    }
+    // the item's parts lie in consecutive CTAs: its start in the first one's second slot, the others in their first
+    constexpr int kPart = paged_part_floats<D, NG>();
+    const int from = paged_share_owner(total, n_act, unit0 + kPagedItemUnits);
+    const int to = paged_share_owner(total, n_act, unit0 + kPagedItemUnits + n_tiles - 1);
+    // parts of a round of the join: half of the ring; `from`'s lies apart from the others
+    constexpr int kRound = kStages * paged_stage_bytes<D>() / 2 / (kPart * 4);
+    auto fetch = [&](int r) {                                      // one thread: round r, if there is one
+      const int q0 = r * kRound, n = min(kRound, to - from + 1 - q0);
+      if (n <= 0) return;
+      const uint32_t dst = base + (r & 1) * kRound * kPart * 4;
+      mbar_expect_tx(bar_join(r & 1), (uint32_t)n * kPart * 4);
+      if (q0 == 0) bulk_load(dst, a.part + ((long long)gridDim.x + from) * kPart, kPart * 4, bar_join(0));
+      const int skip = q0 == 0 ? 1 : 0;
+      if (n > skip) bulk_load(dst + skip * kPart * 4, a.part + (long long)(from + q0 + skip) * kPart, (uint32_t)(n - skip) * kPart * 4, bar_join(r & 1));
+    };
+    if (warp == 0) {
+      float* dst = a.part + ((t0 == 0 ? (long long)gridDim.x : 0) + cta) * kPart;
+#pragma unroll
+      for (int i = 0; i < NG * MT; ++i) {
+        const float* v = o[i / MT][i % MT];
+        reinterpret_cast<float4*>(dst)[i * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
+      }
+      if (g == 0) {
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng)
+          reinterpret_cast<float4*>(dst + NG * 8 * D)[ng * 4 + c] = make_float4(m[ng][0], m[ng][1], l[ng][0], l[ng][1]);
+      }
+      __syncwarp();
+      if (lane == 0) {
+        // the part is visible before the count goes up, and who counts last sees the others'
+        const int last = atom_add_acq_rel(a.tickets + item, 1) == to - from;
+        *s_last = last;
+        if (last) {
+          a.tickets[item] = 0;                                     // ready for the next call
+          if (!more) {
+            fence_proxy_async_global();                            // the parts are read by bulk copies, which
+            fence_proxy_async_smem();                              // overwrite tiles that all warps have done with
+            fetch(0);
+            fetch(1);
+          }
+        }
+      }
+    }
+    paged_consumers_sync();
+    if (*s_last) {
+      clear();
+      auto join = [&](auto ml_of, auto v_of) {                     // adds one part
+        float f[NG][2], e[NG][2];
+#pragma unroll
+        for (int ng = 0; ng < NG; ++ng) {
+          const float4 ml = ml_of(ng);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float top = x ? ml.y : ml.x, now = fmaxf(m[ng][x], top), ref = now == -INFINITY ? 0.f : now;
+            f[ng][x] = exp2f(m[ng][x] - ref);
+            e[ng][x] = exp2f(top - ref);
+            l[ng][x] = fmaf(x ? ml.w : ml.z, e[ng][x], l[ng][x] * f[ng][x]);
+            m[ng][x] = now;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < NG * MT; ++i) {
-          const float* v = o[i / MT][i % MT];
-          reinterpret_cast<float4*>(dst)[i * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
+          const float4 v = v_of(i);
+          float* t = o[i / MT][i % MT];
+          const float *fn = f[i / MT], *en = e[i / MT];
+          t[0] = fmaf(v.x, en[0], t[0] * fn[0]);
+          t[1] = fmaf(v.y, en[1], t[1] * fn[1]);
+          t[2] = fmaf(v.z, en[0], t[2] * fn[0]);
+          t[3] = fmaf(v.w, en[1], t[3] * fn[1]);
         }
-        if (g == 0) {
-#pragma unroll
-          for (int ng = 0; ng < NG; ++ng)
-            reinterpret_cast<float4*>(dst + NG * 8 * D)[ng * 4 + c] = make_float4(m[ng][0], m[ng][1], l[ng][0], l[ng][1]);
-        }
-        __syncwarp();
-        if (lane == 0) {
-          __threadfence();                                         // the part is visible before the count goes up
-          const int last = atomicAdd(a.tickets + item, 1) == to - from;
-          if (last) {
-            a.tickets[item] = 0;                                   // ready for the next call
-            __threadfence();                                       // the other CTAs' parts are visible from here on
-          }
-          *s_last = last;
-        }
-      }
-      paged_consumers_sync();
-      if (*s_last) {
-        clear();
-        for (int q = from + warp; q <= to; q += kPagedWarps) {
-          const float* src = a.part + ((long long)q * 2 + (q == from ? 1 : 0)) * kPart;
-          float4 ml[NG], v[NG * MT];
-#pragma unroll
-          for (int ng = 0; ng < NG; ++ng) ml[ng] = __ldcg(reinterpret_cast<const float4*>(src + NG * 8 * D) + ng * 4 + c);
-#pragma unroll
-          for (int i = 0; i < NG * MT; ++i) v[i] = __ldcg(reinterpret_cast<const float4*>(src) + i * 32 + lane);
-#pragma unroll
-          for (int ng = 0; ng < NG; ++ng) {
-            const float now_a = fmaxf(m[ng][0], ml[ng].x), now_b = fmaxf(m[ng][1], ml[ng].y);
-            const float ref_a = now_a == -INFINITY ? 0.f : now_a, ref_b = now_b == -INFINITY ? 0.f : now_b;
-            const float fa = exp2f(m[ng][0] - ref_a), fb = exp2f(m[ng][1] - ref_b);
-            const float ga = exp2f(ml[ng].x - ref_a), gb = exp2f(ml[ng].y - ref_b);
-            l[ng][0] = fmaf(ml[ng].z, ga, l[ng][0] * fa);
-            l[ng][1] = fmaf(ml[ng].w, gb, l[ng][1] * fb);
-            m[ng][0] = now_a;
-            m[ng][1] = now_b;
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              const float4 x = v[ng * MT + mt];
-              o[ng][mt][0] = fmaf(x.x, ga, o[ng][mt][0] * fa);
-              o[ng][mt][1] = fmaf(x.y, gb, o[ng][mt][1] * fb);
-              o[ng][mt][2] = fmaf(x.z, ga, o[ng][mt][2] * fa);
-              o[ng][mt][3] = fmaf(x.w, gb, o[ng][mt][3] * fb);
+      };
+      if (!more) {
+        // the ring is free: parts arrive in its halves in turn
+        for (int r = 0; r * kRound <= to - from; ++r) {
+          const int n = min(kRound, to - from + 1 - r * kRound);
+          const bool landed = mbar_wait(bar_join(r & 1), (uint32_t)(r >> 1) & 1u);
+          if (!__all_sync(0xffffffffu, landed)) {
+            if (lane == 0) record_status(p.status, kStatusTimeout);
+          } else {
+            for (int q = warp; q < n; q += kPagedWarps) {
+              const float4* src = reinterpret_cast<const float4*>(gen + (r & 1) * kRound * kPart * 4) + q * (kPart / 4);
+              join([&](int ng) { return src[NG * 2 * D + ng * 4 + c]; }, [&](int i) { return src[i * 32 + lane]; });
             }
           }
+          paged_consumers_sync();                                  // the half is read
+          if (tid == 0) {
+            fence_proxy_async_smem();
+            fetch(r + 2);
+          }
         }
-        merge_warps();
-        if (warp == 0) finish(w.b, w.head);
+      } else {
+        for (int q = from + warp; q <= to; q += kPagedWarps) {
+          const float4* src = reinterpret_cast<const float4*>(a.part + ((q == from ? (long long)gridDim.x : 0) + q) * kPart);
+          join([&](int ng) { return __ldcg(src + NG * 2 * D + ng * 4 + c); }, [&](int i) { return __ldcg(src + i * 32 + lane); });
+        }
       }
-      paged_consumers_sync();                                      // s_last is read
+      merge_warps();
+      if (warp == 0) finish(b, head);
     }
-    left -= n;
-    if (left > 0) w.next_item(p, heads);
+    paged_consumers_sync();                                        // s_last is read
   }
 }
 
-// Adds the group's attention to the entries' weights, from the scores and normalisers of paged_attn_kernel. The tiles of all
-// KV heads are cut into equal shares, one per warp; a lane has two entries of a tile.
-__global__ void __launch_bounds__(256) paged_weights_kernel(const PagedAttnArgs a) {
+// Adds the group's attention to the entries' weights, from the scores and normalisers of paged_attn_kernel, which also wrote down
+// whose each tile of scores is. A lane reads four heads' scores of an entry at a time, a warp 512 bytes in a row (an entry per lane,
+// head after head, fetched every sector four times over: 21 us for 131,000 entries of four KV heads); Gs / 4 lanes share an
+// entry and add up. A warp has two such reads, a Gs / 4th of a tile. The rest is a chain of round trips: what a tile is, with its scores; the
+// entries' pages and the normalisers; the old weights, which the attention kernel's producers have asked the L2 cache for.
+constexpr int kPagedWeightsCtas = 5;                       // per SM
+__global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(const PagedAttnArgs a) {
+  const PagedPool& p = a.pool;
+  const int lane = threadIdx.x & 31, share = a.Gs / 4, share_shift = 31 - __clz(share);   // lanes of an entry, parts of a tile
+  const int quad = lane & (share - 1);                     // heads 4 quad .. 4 quad + 3
   grid_dependency_wait();
   allow_dependents();
-  const PagedPool& p = a.pool;
-  const int lane = threadIdx.x & 31;
-  int mine;
-  const int total = paged_total(p, lane, mine) * p.H;
-  const int n_warps = (int)gridDim.x * 8, n_act = min(total, n_warps), me = blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (me >= n_act) return;
-  const int begin = paged_share_begin(total, n_act, me);
-  int left = paged_share_begin(total, n_act, me + 1) - begin;
-  PagedWalk w = paged_seek(p, lane, mine, p.H, begin);
-  while (left > 0) {
-    const int n = min(left, w.n_tiles - w.tile);
-    const float* z = a.lse2 + ((long long)w.b * p.H + w.head) * a.G;
-    for (int t = w.tile; t < w.tile + n; ++t) {
-      const int tile = w.before * p.H + w.head * w.n_tiles + t;
-      if (tile >= a.score_tiles) {                                 // pages that several sequences share: not for accumulating caches
-        if (lane == 0) record_status(p.status, kStatusCapacity);
-        return;
-      }
+  const int total = *a.score_units;
+  const long long parts = (long long)a.score_tiles << share_shift;
+  auto load = [&](long long part, int2& at, float4 (&x)[2]) {        // behind the units in use lies what an earlier call left
+    part = part < parts ? part : parts - 1;
+    at = __ldcg(a.score_at + (part >> share_shift));
+    const float4* src = reinterpret_cast<const float4*>(a.scores) + part * 64 + lane;
+    x[0] = __ldcg(src);
+    x[1] = __ldcg(src + 32);
+  };
+  long long part = blockIdx.x * 8 + (threadIdx.x >> 5);
+  int2 at_next;
+  float4 x_next[2];
+  load(part, at_next, x_next);
+  const long long n_parts = (long long)min(total, a.score_tiles) << share_shift;
+  for (; part < n_parts; part += gridDim.x * 8) {
+    const int2 at = at_next;
+    const float4 x[2] = {x_next[0], x_next[1]};
+    load(part + gridDim.x * 8, at_next, x_next);
+    const int b = at.x & 0xFFFF, h = (int)((unsigned)at.x >> 16);
+    if (at.y < 0 || b >= p.n_seqs || h >= p.H) continue;   // a unit of an item itself, or the attention gave up
+    const float* z = a.lse2 + ((long long)b * p.H + h) * a.G;
+    const int len = p.length(b), first = at.y * kDecTile + ((int)(part & (share - 1)) * 64 + lane) / share;
+    int page[2];
+    float zz[4], *dst[2], old[2];
+    bool ok[2];
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int i = t * kDecTile + k * 32 + lane;
-        if (i >= w.len) continue;
-        const int page = p.page(w.b, i);
-        if ((unsigned)page >= (unsigned)p.n_pages) continue;       // recorded by the attention
-        float* dst = a.weights + (((long long)page * p.H + w.head) << p.page_shift) + (i & (p.page_size() - 1));
-        const float* x = a.scores + ((long long)tile * kDecTile + k * 32 + lane) * a.Gs;
-        float sum = 0.f;
-        for (int hg = 0; hg < a.G; hg += 2) {                      // heads in order: the same sums every time
-          const float2 y = *reinterpret_cast<const float2*>(x + hg);
-          sum += exp2f(y.x - z[hg]);
-          if (hg + 1 < a.G) sum += exp2f(y.y - z[hg + 1]);
-        }
-        *dst += sum;
-      }
+    for (int k = 0; k < 2; ++k) page[k] = p.page(b, min(first + k * 32 / share, (p.max_pages << p.page_shift) - 1));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) zz[j] = z[min(4 * quad + j, a.G - 1)];   // through L1: thousands of warps ask for the same few
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int i = first + k * 32 / share;
+      ok[k] = i < len && (unsigned)page[k] < (unsigned)p.n_pages && quad == 0;   // bad pages were recorded by the attention
+      dst[k] = a.weights + (ok[k] ? (((long long)page[k] * p.H + h) << p.page_shift) + (i & (p.page_size() - 1)) : 0);
+      old[k] = *dst[k];
     }
-    left -= n;
-    if (left > 0) w.next_item(p, p.H);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float e[4] = {exp2f(x[k].x - zz[0]), exp2f(x[k].y - zz[1]), exp2f(x[k].z - zz[2]), exp2f(x[k].w - zz[3])};
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) if (4 * quad + j < a.G) sum += e[j];
+      for (int off = 1; off < share; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      if (ok[k]) *dst[k] = old[k] + sum;
+    }
   }
+  if (total > a.score_tiles && blockIdx.x == 0 && threadIdx.x == 0) record_status(p.status, kStatusCapacity);   // sequences share pages: not for caches with weights
 }
 
 }  // namespace lkv

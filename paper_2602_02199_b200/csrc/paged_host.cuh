@@ -14,8 +14,10 @@ struct laser_kv_paged_ctx {
   float* part = nullptr;
   float* lse2 = nullptr;
   float* scores = nullptr;
+  int2* score_at = nullptr;
   int2* moves = nullptr;
   int group, head_blocks, n_wide;           // query heads per KV head; blocks of 8 * n_wide of them
+  int score_heads = 0;                      // scores of an entry
   int score_tiles = 0;
   long long n_moves = 0, cap = 0;
   int num_sms = 1;
@@ -24,12 +26,12 @@ struct laser_kv_paged_ctx {
 
 namespace {
 
-constexpr int kPagedMaxCtas = 320;          // upper bound of the attention's persistent grid
+constexpr int paged_max_ctas(int d) { return d == 64 ? 480 : d == 128 ? 320 : 160; }   // upper bounds of the attention's persistent grid
 
 struct PagedDerived {
-  int group, n_wide, head_blocks, page_shift, score_tiles;
+  int group, n_wide, head_blocks, page_shift, score_tiles, score_heads;
   long long cap, n_moves;
-  size_t append_tickets, attn_tickets, part, lse2, scores, moves, zeroed, total;
+  size_t append_tickets, attn_tickets, part, lse2, scores, score_at, moves, zeroed, total;
 };
 
 laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d) {
@@ -51,27 +53,31 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
   d->group = c->n_q_heads / c->n_kv_heads;
   d->n_wide = c->head_dim == 256 || d->group <= 8 ? 1 : 2;
   d->head_blocks = (d->group + 8 * d->n_wide - 1) / (8 * d->n_wide);
-  const long long seq_tiles = (d->cap + kDecTile - 1) / kDecTile;
+  const long long seq_tiles = (d->cap + kDecTile - 1) / kDecTile + kPagedItemUnits;
   if (c->n_seqs > 65535 || c->n_kv_heads > 65535 || d->cap > (1ll << 30) || rows > 0x7fffffffLL ||
       (double)c->n_seqs * c->n_kv_heads * d->head_blocks * (double)seq_tiles > 2147483647.0 ||
       (double)c->n_seqs * c->n_q_heads > 2147483647.0)
     return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: more than 65535 sequences or KV heads, 2^30 entries per sequence or 2^31 rows or tiles");
   for (d->page_shift = 3; (1 << d->page_shift) < c->page_size;) ++d->page_shift;
   // Pages that no two sequences share bound the entries of all sequences together.
-  const long long all = (long long)c->n_seqs * seq_tiles, pooled = (long long)c->n_pages * c->page_size / kDecTile + c->n_seqs;
+  const long long all = (long long)c->n_seqs * seq_tiles, pooled = (long long)c->n_pages * c->page_size / kDecTile + (1 + kPagedItemUnits) * (long long)c->n_seqs;
   const long long tiles = (all < pooled ? all : pooled) * c->n_kv_heads;
   if (tiles > 0x7fffffffLL) return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: too many entries");
   d->score_tiles = c->track_weights ? (int)tiles : 0;
   d->n_moves = c->track_weights ? rows / 2 + 1 : 0;
+  for (d->score_heads = 4; d->score_heads < d->group;) d->score_heads *= 2;
+  if (c->track_weights && d->group > 128)
+    return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: weights for at most 128 query heads per KV head");
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes); return o; };
-  take(256);                                                   // status word, ticket of the eviction
+  take(256);                                                   // status word, ticket of the eviction, units of the last accumulating call
   d->append_tickets = take((size_t)c->n_seqs * 4);
   d->attn_tickets = take((size_t)c->n_seqs * c->n_kv_heads * d->head_blocks * 4);
   d->zeroed = off;
-  d->part = take((size_t)kPagedMaxCtas * 2 * d->n_wide * 8 * (c->head_dim + 2) * sizeof(float));
+  d->part = take((size_t)paged_max_ctas(c->head_dim) * 2 * d->n_wide * 8 * (c->head_dim + 2) * sizeof(float));
   d->lse2 = take(c->track_weights ? (size_t)c->n_seqs * c->n_q_heads * 4 : 0);
-  d->scores = take((size_t)d->score_tiles * kDecTile * ((d->group + 1) / 2 * 2) * sizeof(float));
+  d->scores = take((size_t)d->score_tiles * kDecTile * d->score_heads * sizeof(float));
+  d->score_at = take((size_t)d->score_tiles * sizeof(int2));
   d->moves = take((size_t)d->n_moves * sizeof(int2));
   d->total = off;
   return LASER_KV_OK;
@@ -144,7 +150,7 @@ cudaError_t launch_paged_attn(const laser_kv_paged_ctx* h, const PagedAttnArgs& 
   if (e != cudaSuccess) return e;
   const long long most = (long long)h->cfg.n_seqs * h->cfg.n_kv_heads * h->head_blocks * ((h->cap + kDecTile - 1) / kDecTile);
   long long grid = (long long)h->num_sms * paged_ctas_per_sm<D>();
-  if (grid > kPagedMaxCtas) grid = kPagedMaxCtas;
+  if (grid > paged_max_ctas(D)) grid = paged_max_ctas(D);
   if (grid > most) grid = most;
   return launch(paged_attn_kernel<HALF, D, NG>, dim3((unsigned)grid), kPagedThreads, paged_smem_bytes<D, NG>(), st, true, h->map_k, h->map_v, a);
 }
@@ -232,12 +238,14 @@ laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* 
   if (weights) {
     h->lse2 = reinterpret_cast<float*>(ws + d.lse2);
     h->scores = reinterpret_cast<float*>(ws + d.scores);
+    h->score_at = reinterpret_cast<int2*>(ws + d.score_at);
     h->moves = reinterpret_cast<int2*>(ws + d.moves);
   }
   h->group = d.group;
   h->head_blocks = d.head_blocks;
   h->n_wide = d.n_wide;
   h->score_tiles = d.score_tiles;
+  h->score_heads = d.score_heads;
   h->n_moves = d.n_moves;
   h->cap = d.cap;
   h->num_sms = sms;
@@ -326,12 +334,14 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
   a.part = h->part;
   a.tickets = h->attn_tickets;
   a.G = h->group;
-  a.Gs = (h->group + 1) / 2 * 2;
+  a.Gs = h->score_heads;
   a.head_blocks = h->head_blocks;
   a.scale_log2e = (softmax_scale == 0.f ? 1.0f / std::sqrt((float)h->cfg.head_dim) : softmax_scale) * 1.4426950408889634f;
   if (accumulate) {
     a.lse2 = h->lse2;
     a.scores = h->scores;
+    a.score_at = h->score_at;
+    a.score_units = reinterpret_cast<int*>(h->ws) + 2;
     a.score_tiles = h->score_tiles;
     a.weights = h->rows.weights;
   }
@@ -339,8 +349,8 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
   cudaError_t e = h->cfg.dtype == LASER_KV_FP16 ? launch_paged_attn_t<true>(h, a, st) : launch_paged_attn_t<false>(h, a, st);
   if (e != cudaSuccess) return fail(nullptr, LASER_KV_ERR_CUDA, "paged_attn_kernel launch: %s", cudaGetErrorString(e));
   if (accumulate) {
-    long long grid = ((long long)h->score_tiles + 7) / 8;
-    if (grid > 4ll * h->num_sms) grid = 4ll * h->num_sms;
+    long long grid = ((long long)h->score_tiles * (a.Gs / 4) + 7) / 8;   // a warp a part
+    if (grid > (long long)kPagedWeightsCtas * h->num_sms) grid = (long long)kPagedWeightsCtas * h->num_sms;
     e = launch(paged_weights_kernel, dim3((unsigned)grid), 256, 0, st, true, a);
     if (e != cudaSuccess) return fail(nullptr, LASER_KV_ERR_CUDA, "paged_weights_kernel launch: %s", cudaGetErrorString(e));
   }

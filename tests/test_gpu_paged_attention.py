@@ -26,6 +26,7 @@ EDGES = [0, 1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 1000]
     (256, 9, 1, 8, False, [129, 5, 0]),
     (128, 1, 5, 32, False, [0, 0, 0]),                    # nothing at all
     (128, 3, 1, 16, True, [5000, 0, 1, 64]),
+    (64, 70, 1, 16, False, [100, 3000]),                  # five readings, more heads than a warp has lanes
 ])
 def test_attention_against_64_bits(dtype, D, G, H, page_size, token_major, lens):
     cache, gen = build(lens, H=H, G=G, D=D, page_size=page_size, dtype=dtype, token_major=token_major)
@@ -46,8 +47,9 @@ def test_many_sequences(dtype, n):
 @pytest.mark.parametrize("D,H,lens", [(64, 1, [200001]), (128, 1, [70000, 3, 33333]), (256, 2, [20011])])
 def test_long_caches_are_split_and_joined(D, H, lens):
     for dtype in ("bf16", "fp16"):
-        cache, gen = build(lens, H=H, G=4, D=D, page_size=64, dtype=dtype)
-        check_attention(cache, queries(cache, gen, 3.0), accumulate=True)
+        for G in (4, 13):
+            cache, gen = build(lens, H=H, G=G, D=D, page_size=64, dtype=dtype)
+            check_attention(cache, queries(cache, gen, 3.0), accumulate=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])

@@ -28,7 +28,7 @@ def _message():
     (dict(head_dim=96), Bn.ERR_UNSUPPORTED), (dict(head_dim=512), Bn.ERR_UNSUPPORTED), (dict(page_size=4), Bn.ERR_UNSUPPORTED),
     (dict(page_size=24), Bn.ERR_UNSUPPORTED), (dict(page_size=8192), Bn.ERR_UNSUPPORTED), (dict(dtype=2), Bn.ERR_INVALID_ARG),
     (dict(track_weights=2), Bn.ERR_INVALID_ARG), (dict(n_seqs=65536), Bn.ERR_UNSUPPORTED), (dict(max_pages=1 << 27), Bn.ERR_UNSUPPORTED),
-    (dict(n_pages=1 << 28), Bn.ERR_UNSUPPORTED), (dict(n_seqs=60000, max_pages=1 << 17), Bn.ERR_UNSUPPORTED)])
+    (dict(n_pages=1 << 28), Bn.ERR_UNSUPPORTED), (dict(n_q_heads=8 * 129), Bn.ERR_UNSUPPORTED), (dict(n_seqs=60000, max_pages=1 << 17), Bn.ERR_UNSUPPORTED)])
 def test_configurations_out_of_range_are_refused(change, status):
     with pytest.raises(Bn.LaserKVError) as e:
         Bn.laser_kv_paged_query_sizes(_cfg(**change))
@@ -45,11 +45,13 @@ def test_workspace_sizes(group, track, d):
     cfg = _cfg(n_q_heads=8 * group, head_dim=d, track_weights=track)
     size = Bn.laser_kv_paged_query_sizes(cfg)
     assert size % 256 == 0
-    # parts of 320 CTAs at most, and with weights a score per query head and entry, a pair of indices per two
-    wide = 1 if d == 256 or group <= 8 else 2
-    least = 320 * 2 * wide * 8 * (d + 2) * 4
+    # parts of the CTAs, and with weights a score per query head (a power of two of them) and entry, a pair of indices per two
+    wide, ctas = 1 if d == 256 or group <= 8 else 2, {64: 480, 128: 320, 256: 160}[d]
+    least = ctas * 2 * wide * 8 * (d + 2) * 4
     if track:
-        least += (64 * 16 // 64 + 4) * 8 * 64 * ((group + 1) // 2 * 2) * 4 + 64 * 16 * 8 // 2 * 8
+        heads = max(4, 1 << (group - 1).bit_length())
+        units = (64 * 16 // 64 + 3 * 4) * 8
+        least += units * (64 * heads * 4 + 8) + 64 * 16 * 8 // 2 * 8
     assert least <= size <= least + 20000
 
 
