@@ -510,8 +510,8 @@ enum { LASER_KV_BF16 = 0, LASER_KV_FP16 = 1 };
 typedef struct {
   int32_t n_seqs;              /* rows of the table, at most 65535                               */
   int32_t n_q_heads;           /* H_q                                                            */
-  int32_t n_kv_heads;          /* H_kv; H_q % H_kv == 0. Up to 16 query heads per KV head (8 of head_dim 256) share one reading of
-                                  the cache, more read it several times                        */
+  int32_t n_kv_heads;          /* H_kv; H_q % H_kv == 0. Up to 16 query heads per KV head share one reading of the cache, more
+                                  read it several times; with weights at most 128 of them       */
   int32_t head_dim;            /* 64, 128 or 256                                                 */
   int32_t page_size;           /* entries of a page: a power of two from 8 to 4096               */
   int32_t n_pages;             /* pages of the pool                                              */

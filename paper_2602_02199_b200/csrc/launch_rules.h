@@ -138,14 +138,20 @@ LKV_HOST_DEVICE inline int paged_shares(int total, int grid) {
   return n < grid ? n : grid;
 }
 
-// CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: as many as fill the SMs once, of a thousand
-// entries at least, of at most kEvictKeys (their sort keys stay in shared memory). 0: more entries than `most` CTAs hold.
-constexpr int kEvictKeys = 49152;
+// CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: at most kEvictKeys each (their sort keys stay in
+// shared memory), kEvictOwn where the SMs have room for two CTAs each. 0: more entries than `most` CTAs hold.
+constexpr int kEvictKeys = 49152, kEvictOwn = 4096;
 inline int evict_cluster(int num_sms, long long heads, long long cap, int most) {
   int n = 1;
-  while (n < most && 2 * n * heads <= num_sms && cap > 1024ll * n) n *= 2;
+  while (n < most && 2 * n * heads <= 2ll * num_sms && cap > (long long)kEvictOwn * n) n *= 2;
   while (n < most && cap > (long long)kEvictKeys * n) n *= 2;
   return cap > (long long)kEvictKeys * n ? 0 : n;
+}
+
+// CTAs that move the rows of one (sequence, KV head), of at most `moves`: 32 rows each, up to eight CTAs per SM in all.
+inline int move_ctas(int num_sms, long long heads, long long moves) {
+  const long long n = (moves + 31) / 32, room = 8ll * num_sms / heads;
+  return (int)(n < room ? (n > 0 ? n : 1) : room > 0 ? room : 1);
 }
 
 }  // namespace lkv

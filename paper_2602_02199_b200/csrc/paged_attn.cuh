@@ -81,7 +81,7 @@ template <int D, int NG>
 __host__ __device__ constexpr int paged_part_floats() { return NG * 8 * (D + 2); }
 template <int D, int NG>
 __host__ __device__ constexpr uint32_t paged_smem_bytes() {
-  return 1024u + paged_stages<D>() * paged_stage_bytes<D>() + 2u * D / 16 * 512u + 2u * kPagedWarps * NG * 8u * 4u + (2u * paged_stages<D>() + 2u) * 8u + 16u;
+  return 1024u + paged_stages<D>() * paged_stage_bytes<D>() + 2u * D / 16 * 512u + 2u * kPagedWarps * 8u * 4u + (2u * paged_stages<D>() + 2u) * 8u + 16u;
 }
 
 // D (16x8, fp32) += A (16x16, row) * B (16x8, col)
@@ -198,6 +198,9 @@ __device__ __forceinline__ void tma_load_4d_once(uint32_t dst, const CUtensorMap
       "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "l"(policy)
       : "memory");
 }
+__device__ __forceinline__ void st_shared_zero(uint32_t addr) {
+  asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(addr), "r"(0) : "memory");
+}
 __device__ __forceinline__ void prefetch_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 __device__ __forceinline__ int atom_add_acq_rel(int* p, int v) {
   int old;
@@ -214,9 +217,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   const uint32_t base = (smem_u32(psm_raw) + 1023u) & ~1023u;
   uint8_t* const gen = psm_raw + (base - smem_u32(psm_raw));
   float4* const red = reinterpret_cast<float4*>(gen + kStages * paged_stage_bytes<D>());   // [2][MT][32]: merge of the warps
-  float* const wm = reinterpret_cast<float*>(red + 2 * MT * 32);                           // [warps][NG * 8] maxima
-  float* const wl = wm + kPagedWarps * NG * 8;                                             // sums
-  int* const s_last = reinterpret_cast<int*>(wl + kPagedWarps * NG * 8);
+  float* const wm = reinterpret_cast<float*>(red + 2 * MT * 32);                           // [warps][8] maxima
+  float* const wl = wm + kPagedWarps * 8;                                                  // sums
+  int* const s_last = reinterpret_cast<int*>(wl + kPagedWarps * 8);
   const uint32_t bars = smem_u32(s_last) + 16u;
   auto bar_full = [&](int s) { return bars + 8u * s; };
   auto bar_empty = [&](int s) { return bars + 8u * (kStages + s); };
@@ -304,7 +307,28 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   }
 
   // ---- consumers ------------------------------------------------------------------------------------
+  // With one set of eight heads a warp has 16 rows of every tile; with two, a pair of warps has a set, a warp of it 32 rows, 16
+  // at a time: a warp's registers hold eight heads either way.
+  constexpr int kTeam = kPagedWarps / NG;                          // warps of a set
   const int g = lane >> 2, c = lane & 3;                           // fragment coordinates, as in decode_split_kernel
+  const int team = warp / kTeam, mate = warp % kTeam;
+  auto first_head = [&](int head, int h) { return ((head - h * a.head_blocks) * NG + team) * 8; };   // of the warp's set, in the group
+
+  uint32_t qb[MT][2];                                              // B fragments of Q^T, heads past G are zero
+  auto load_q = [&]() {                                            // without a condition, so that all loads are under way together
+    const int h = w.head / a.head_blocks, hg = first_head(w.head, h) + g;
+    const uint32_t keep = hg < a.G ? 0xFFFFFFFFu : 0u;
+    const uint16_t* q = a.Q + w.b * a.qs_b + ((long long)h * a.G + min(hg, a.G - 1)) * a.qs_h + 2 * c;
+#pragma unroll
+    for (int ks = 0; ks < MT; ++ks) {
+      qb[ks][0] = *reinterpret_cast<const uint32_t*>(q + 16 * ks);
+      qb[ks][1] = *reinterpret_cast<const uint32_t*>(q + 16 * ks + 8);
+    }
+#pragma unroll
+    for (int ks = 0; ks < MT; ++ks) { qb[ks][0] &= keep; qb[ks][1] &= keep; }
+  };
+  if (more) load_q();
+
   // rows without entries
   for (int b = cta; b < p.n_seqs; b += gridDim.x) {
     if (p.length(b) != p.lens[b] && tid == 0) record_status(p.status, kPagedBadPage);
@@ -320,128 +344,102 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     if (a.lse) for (int i = tid; i < p.H * a.G; i += kPagedWarps * 32) a.lse[(long long)b * p.H * a.G + i] = -INFINITY;
   }
 
-  float o[NG][MT][4], m[NG][2], l[NG][2];
-  // the warps' results are combined in warp 0: sums in a fixed order
+  float o[MT][4], m[2], l[2];
+  auto clear = [&]() {
+    m[0] = m[1] = -INFINITY;
+    l[0] = l[1] = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[mt][i] = 0.f;
+  };
+  // the results of a team's warps are combined in its first one: sums in a fixed order
   auto merge_warps = [&]() {
     if (g == 0) {
 #pragma unroll
-      for (int ng = 0; ng < NG; ++ng)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          wm[warp * NG * 8 + ng * 8 + 2 * c + x] = m[ng][x];
-          wl[warp * NG * 8 + ng * 8 + 2 * c + x] = l[ng][x];
-        }
+      for (int x = 0; x < 2; ++x) {
+        wm[warp * 8 + 2 * c + x] = m[x];
+        wl[warp * 8 + 2 * c + x] = l[x];
+      }
     }
     paged_consumers_sync();
 #pragma unroll
-    for (int ng = 0; ng < NG; ++ng)
+    for (int x = 0; x < 2; ++x) {
+      const int at = team * kTeam * 8 + 2 * c + x;
+      float top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int at = ng * 8 + 2 * c + x;
-        float top = -INFINITY, sum = 0.f;
+      for (int wi = 0; wi < kTeam; ++wi) top = fmaxf(top, wm[wi * 8 + at]);
+      const float ref = top == -INFINITY ? 0.f : top;              // nothing above -inf: all factors are 0
 #pragma unroll
-        for (int wi = 0; wi < kPagedWarps; ++wi) top = fmaxf(top, wm[wi * NG * 8 + at]);
-        const float ref = top == -INFINITY ? 0.f : top;            // nothing above -inf: all factors are 0
+      for (int wi = 0; wi < kTeam; ++wi) sum = fmaf(wl[wi * 8 + at], exp2f(wm[wi * 8 + at] - ref), sum);
+      const float f = exp2f(m[x] - ref);
+      m[x] = top;
+      l[x] = sum;
 #pragma unroll
-        for (int wi = 0; wi < kPagedWarps; ++wi) sum = fmaf(wl[wi * NG * 8 + at], exp2f(wm[wi * NG * 8 + at] - ref), sum);
-        const float f = exp2f(m[ng][x] - ref);
-        m[ng][x] = top;
-        l[ng][x] = sum;
+      for (int mt = 0; mt < MT; ++mt) { o[mt][x] *= f; o[mt][x + 2] *= f; }
+    }
+    auto put = [&](int slot) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) { o[ng][mt][x] *= f; o[ng][mt][x + 2] *= f; }
+      for (int mt = 0; mt < MT; ++mt) red[(slot * MT + mt) * 32 + lane] = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+    };
+    auto add = [&](int slot) {
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        const float4 v = red[(slot * MT + mt) * 32 + lane];
+        o[mt][0] += v.x; o[mt][1] += v.y; o[mt][2] += v.z; o[mt][3] += v.w;
       }
-    // through a buffer that holds 8 heads of two warps at a time
-#pragma unroll
-    for (int ng = 0; ng < NG; ++ng) {
-      auto put = [&](int slot) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
-          red[(slot * MT + mt) * 32 + lane] = make_float4(o[ng][mt][0], o[ng][mt][1], o[ng][mt][2], o[ng][mt][3]);
-      };
-      auto add = [&](int slot) {
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          const float4 v = red[(slot * MT + mt) * 32 + lane];
-          o[ng][mt][0] += v.x; o[ng][mt][1] += v.y; o[ng][mt][2] += v.z; o[ng][mt][3] += v.w;
-        }
-      };
-      if (ng > 0) paged_consumers_sync();
+    };
+    if constexpr (NG == 1) {
       if (warp >= 2) put(warp - 2);
       paged_consumers_sync();
       if (warp < 2) add(warp);
       if (warp == 1) put(1);
       paged_consumers_sync();
       if (warp == 0) add(1);
+    } else {
+      if (mate == 1) put(team);
+      paged_consumers_sync();
+      if (mate == 0) add(team);
     }
   };
-  auto finish = [&](int b, int head) {                             // warp 0: the item's results
-    const int h = head / a.head_blocks, first = (head - h * a.head_blocks) * NG * 8;
+  auto finish = [&](int b, int head) {                             // a team's first warp: its heads' results
+    const int h = head / a.head_blocks;
 #pragma unroll
-    for (int ng = 0; ng < NG; ++ng)
+    for (int x = 0; x < 2; ++x) {
+      const int hg = first_head(head, h) + 2 * c + x;
+      if (hg >= a.G) continue;
+      const long long row = ((long long)b * p.H + h) * a.G + hg;
+      const float inv = 1.f / l[x];
+      if (a.out16) {
+        uint16_t* dst = static_cast<uint16_t*>(a.out) + row * D + g;
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int hg = first + ng * 8 + 2 * c + x;
-        if (hg >= a.G) continue;
-        const long long row = ((long long)b * p.H + h) * a.G + hg;
-        const float inv = 1.f / l[ng][x];
-        if (a.out16) {
-          uint16_t* dst = static_cast<uint16_t*>(a.out) + row * D + g;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            const uint32_t y = paged_pack<HALF>(o[ng][mt][x] * inv, o[ng][mt][x + 2] * inv);
-            dst[16 * mt] = (uint16_t)y;
-            dst[16 * mt + 8] = (uint16_t)(y >> 16);
-          }
-        } else {
-          float* dst = static_cast<float*>(a.out) + row * D + g;
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt) {
-            dst[16 * mt] = o[ng][mt][x] * inv;
-            dst[16 * mt + 8] = o[ng][mt][x + 2] * inv;
-          }
+        for (int mt = 0; mt < MT; ++mt) {
+          const uint32_t y = paged_pack<HALF>(o[mt][x] * inv, o[mt][x + 2] * inv);
+          dst[16 * mt] = (uint16_t)y;
+          dst[16 * mt + 8] = (uint16_t)(y >> 16);
         }
-        if (g == 0) {
-          const float z = m[ng][x] + log2f(l[ng][x]);
-          if (a.lse) a.lse[row] = z * 0.6931471805599453f;
-          if (a.lse2) a.lse2[row] = z;
+      } else {
+        float* dst = static_cast<float*>(a.out) + row * D + g;
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          dst[16 * mt] = o[mt][x] * inv;
+          dst[16 * mt + 8] = o[mt][x + 2] * inv;
         }
       }
-  };
-  auto clear = [&]() {
-#pragma unroll
-    for (int ng = 0; ng < NG; ++ng) {
-      m[ng][0] = m[ng][1] = -INFINITY;
-      l[ng][0] = l[ng][1] = 0.f;
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[ng][mt][i] = 0.f;
+      if (g == 0) {
+        const float z = m[x] + log2f(l[x]);
+        if (a.lse) a.lse[row] = z * 0.6931471805599453f;
+        if (a.lse2) a.lse2[row] = z;
+      }
     }
   };
 
-  uint32_t qb[NG][MT][2];                                          // B fragments of Q^T, heads past G are zero
-  auto load_q = [&]() {
-    const int h = w.head / a.head_blocks, first = (w.head - h * a.head_blocks) * NG * 8;
-#pragma unroll
-    for (int ng = 0; ng < NG; ++ng) {
-      const int hg = first + ng * 8 + g;
-      const uint16_t* q = a.Q + w.b * a.qs_b + ((long long)h * a.G + hg) * a.qs_h;
-#pragma unroll
-      for (int ks = 0; ks < MT; ++ks) {
-        qb[ng][ks][0] = hg < a.G ? *reinterpret_cast<const uint32_t*>(q + 16 * ks + 2 * c) : 0u;
-        qb[ng][ks][1] = hg < a.G ? *reinterpret_cast<const uint32_t*>(q + 16 * ks + 8 + 2 * c) : 0u;
-      }
-    }
-  };
-  constexpr bool kAhead = NG == 1;                                 // two sets' queries take too many registers during a merge
-  if (kAhead && more) load_q();
   int st = 0, round = 0;
   bool gone = false;                                               // a wait ran out: the list is walked, nothing is computed
   while (more) {
     const int t0 = w.first(begin), t1 = w.last(stop);
     if (t0 >= t1) break;                                           // the share ends with units of the item itself
-    const int h = w.head / a.head_blocks, first = (w.head - h * a.head_blocks) * NG * 8;
-    if (!kAhead) load_q();
+    const int h = w.head / a.head_blocks;
     clear();
     const int score_unit = w.before * p.H + h * w.units();           // of the item
     if (a.scores && tid < (t0 == 0 ? kPagedItemUnits : 0) && score_unit + tid < a.score_tiles) a.score_at[score_unit + tid] = make_int2(0, -1);
@@ -450,100 +448,85 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         if (lane == 0) record_status(p.status, kStatusTimeout);
         gone = true;
       }
-      const int rows = w.len - t * kDecTile - warp * 16;           // of the warp's 16 in this tile
-      if (!gone && rows > 0) {
+#pragma unroll
+      for (int blk = 0; blk < NG; ++blk) {                         // 16 rows
+        const int row0 = mate * (16 * NG) + 16 * blk, rows = w.len - t * kDecTile - row0;   // rows that the sequence has from row0 on
+        if (gone || rows <= 0) continue;
         const uint32_t k_tile = base + st * paged_stage_bytes<D>(), v_tile = k_tile + kHalf;
-        float s[NG][4], s1[NG][4];
-#pragma unroll
-        for (int ng = 0; ng < NG; ++ng)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s[ng][i] = s1[ng][i] = 0.f;
+        float x[4] = {0.f, 0.f, 0.f, 0.f}, x1[4] = {0.f, 0.f, 0.f, 0.f};   // two chains
 #pragma unroll
         for (int ks = 0; ks < MT; ks += 2) {
           uint32_t k0[4], k1[4];
-          ldsm_x4(k_tile + dec_swz(warp * 16 + (lane & 15), 2 * ks + (lane >> 4)), k0);
-          ldsm_x4(k_tile + dec_swz(warp * 16 + (lane & 15), 2 * ks + 2 + (lane >> 4)), k1);
-#pragma unroll
-          for (int ng = 0; ng < NG; ++ng) {
-            paged_mma<HALF>(s[ng], k0, qb[ng][ks][0], qb[ng][ks][1]);
-            paged_mma<HALF>(NG == 1 ? s1[ng] : s[ng], k1, qb[ng][ks + 1][0], qb[ng][ks + 1][1]);   // two chains in all
-          }
+          ldsm_x4(k_tile + dec_swz(row0 + (lane & 15), 2 * ks + (lane >> 4)), k0);
+          ldsm_x4(k_tile + dec_swz(row0 + (lane & 15), 2 * ks + 2 + (lane >> 4)), k1);
+          paged_mma<HALF>(x, k0, qb[ks][0], qb[ks][1]);
+          paged_mma<HALF>(x1, k1, qb[ks + 1][0], qb[ks + 1][1]);
         }
         // rows past the sequence's end hold whatever the page or an earlier tile left there
         const bool v_lo = g < rows, v_hi = g + 8 < rows;
-        uint32_t pb[NG][HALF ? 2 : 3][2];                          // B fragments of P^T, term by term
-        float beta[NG][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v_lo : v_hi) ? (x[i] + x1[i]) * a.scale_log2e : -INFINITY;
+        const int unit = score_unit + kPagedItemUnits + t;
+        if (a.scores && unit < a.score_tiles) {
+          const int hg = first_head(w.head, h) + 2 * c;
+          if (tid == 0 && blk == 0) a.score_at[unit] = make_int2((int)((unsigned)w.b | (unsigned)h << 16), t);
+          float* dst = a.scores + ((long long)unit * kDecTile + row0 + g) * a.Gs + hg;
+          if (hg < a.G) {
+            if (v_lo) *reinterpret_cast<float2*>(dst) = make_float2(x[0], x[1]);
+            if (v_hi) *reinterpret_cast<float2*>(dst + 8 * a.Gs) = make_float2(x[2], x[3]);
+          }
+        }
+        float alpha[2], beta[2];
         bool raise = false;
-        float alpha[NG][2];
 #pragma unroll
-        for (int ng = 0; ng < NG; ++ng) {
-          float x[4];
+        for (int y = 0; y < 2; ++y) {
+          float top = fmaxf(x[y], x[y + 2]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v_lo : v_hi) ? (NG == 1 ? s[ng][i] + s1[ng][i] : s[ng][i]) * a.scale_log2e : -INFINITY;
-          const int unit = score_unit + kPagedItemUnits + t;
-          if (a.scores && unit < a.score_tiles) {
-            const int hg = first + ng * 8 + 2 * c;
-            if (ng == 0 && tid == 0) a.score_at[unit] = make_int2((int)((unsigned)w.b | (unsigned)h << 16), t);
-            float* dst = a.scores + ((long long)unit * kDecTile + warp * 16 + g) * a.Gs + hg;
-            if (hg < a.G) {
-              if (v_lo) *reinterpret_cast<float2*>(dst) = make_float2(x[0], x[1]);
-              if (v_hi) *reinterpret_cast<float2*>(dst + 8 * a.Gs) = make_float2(x[2], x[3]);
-            }
+          for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+          const float ref = top == -INFINITY ? 0.f : top;
+          const float old = m[y], now = fmaxf(old, top), run = now == -INFINITY ? 0.f : now;
+          alpha[y] = exp2f(old - run);
+          beta[y] = exp2f(top - run);
+          raise |= now > old;
+          m[y] = now;
+          x[y] = exp2f(x[y] - ref);
+          x[y + 2] = exp2f(x[y + 2] - ref);
+          l[y] = fmaf(x[y] + x[y + 2], beta[y], l[y] * alpha[y]);
+          if constexpr (HALF) {                                    // exact: powers of two
+            x[y] *= 32768.f;
+            x[y + 2] *= 32768.f;
+            beta[y] *= 1.f / 32768.f;
           }
+        }
+        uint32_t pb[HALF ? 2 : 3][2];                              // B fragments of P^T, term by term
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            float top = fmaxf(x[y], x[y + 2]);
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            const float ref = top == -INFINITY ? 0.f : top;
-            const float old = m[ng][y], now = fmaxf(old, top), run = now == -INFINITY ? 0.f : now;
-            alpha[ng][y] = exp2f(old - run);
-            beta[ng][y] = exp2f(top - run);
-            raise |= now > old;
-            m[ng][y] = now;
-            x[y] = exp2f(x[y] - ref);
-            x[y + 2] = exp2f(x[y + 2] - ref);
-            l[ng][y] = fmaf(x[y] + x[y + 2], beta[ng][y], l[ng][y] * alpha[ng][y]);
-            if constexpr (HALF) {                                  // exact: powers of two
-              x[y] *= 32768.f;
-              x[y + 2] *= 32768.f;
-              beta[ng][y] *= 1.f / 32768.f;
-            }
-          }
-#pragma unroll
-          for (int term = 0; term < (HALF ? 2 : 3); ++term) {
-            const uint32_t lo = paged_pack<HALF>(x[0], x[1]), hi = paged_pack<HALF>(x[2], x[3]);
-            pb[ng][term][0] = movmatrix_trans(lo);
-            pb[ng][term][1] = movmatrix_trans(hi);
-            const float2 f0 = paged_unpack<HALF>(lo), f1 = paged_unpack<HALF>(hi);
-            x[0] -= f0.x; x[1] -= f0.y; x[2] -= f1.x; x[3] -= f1.y;
-          }
+        for (int term = 0; term < (HALF ? 2 : 3); ++term) {
+          const uint32_t lo = paged_pack<HALF>(x[0], x[1]), hi = paged_pack<HALF>(x[2], x[3]);
+          pb[term][0] = movmatrix_trans(lo);
+          pb[term][1] = movmatrix_trans(hi);
+          const float2 f0 = paged_unpack<HALF>(lo), f1 = paged_unpack<HALF>(hi);
+          x[0] -= f0.x; x[1] -= f0.y; x[2] -= f1.x; x[3] -= f1.y;
         }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-          for (int ng = 0; ng < NG; ++ng)
+          for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) o[ng][mt][i] *= alpha[ng][i & 1];
+            for (int i = 0; i < 4; ++i) o[mt][i] *= alpha[i & 1];
         }
-        // values of rows past the end are taken as zeros: 0 times what lies there could be NaN
-        const bool cut = rows < 16;
-        const uint32_t keep_lo = (2 * c < rows ? 0xFFFFu : 0u) | (2 * c + 1 < rows ? 0xFFFF0000u : 0u);
-        const uint32_t keep_hi = (2 * c + 8 < rows ? 0xFFFFu : 0u) | (2 * c + 9 < rows ? 0xFFFF0000u : 0u);
+        if (rows < 16) {                                           // values of rows past the end: 0 times what lies there could be NaN
+          for (int i = rows * (D / 8) + lane; i < 16 * (D / 8); i += 32) st_shared_zero(v_tile + dec_swz(row0 + i / (D / 8), i % (D / 8)));
+          fence_proxy_async_smem();                                // before a later tile is brought here
+          __syncwarp();
+        }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           uint32_t vt[4];
-          ldsm_x4_trans(v_tile + dec_swz(warp * 16 + (lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), vt);
-          if (cut) { vt[0] &= keep_lo; vt[1] &= keep_lo; vt[2] &= keep_hi; vt[3] &= keep_hi; }
+          ldsm_x4_trans(v_tile + dec_swz(row0 + (lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), vt);
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ng = 0; ng < NG; ++ng) {
-            float blk[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int term = 0; term < (HALF ? 2 : 3); ++term) paged_mma<HALF>(sum, vt, pb[term][0], pb[term][1]);
 #pragma unroll
-            for (int term = 0; term < (HALF ? 2 : 3); ++term) paged_mma<HALF>(blk, vt, pb[ng][term][0], pb[ng][term][1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[ng][mt][i] = fmaf(blk[i], beta[ng][i & 1], o[ng][mt][i]);
-          }
+          for (int i = 0; i < 4; ++i) o[mt][i] = fmaf(sum[i], beta[i & 1], o[mt][i]);
         }
       }
       __syncwarp();
@@ -552,22 +535,20 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     }
     // lanes with equal c hold different rows
 #pragma unroll
-    for (int ng = 0; ng < NG; ++ng)
+    for (int x = 0; x < 2; ++x)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1) l[ng][x] += __shfl_xor_sync(0xffffffffu, l[ng][x], off);
+      for (int off = 4; off < 32; off <<= 1) l[x] += __shfl_xor_sync(0xffffffffu, l[x], off);
     // the next item's queries are on their way while this one's results are merged
     const int b = w.b, head = w.head, item = b * heads + head, n_tiles = w.n_tiles, unit0 = w.unit0;
     more = w.next(p, heads, stop) && w.last(stop) > 0;             // not just units of the next item itself
-    if (kAhead && more) load_q();
+    if (more) load_q();
     merge_warps();
     if (t1 - t0 == n_tiles) {
-      if (warp == 0) finish(b, head);
+      if (mate == 0) finish(b, head);
       continue;
     }
     // the item's parts lie in consecutive CTAs: its start in the first one's second slot, the others in their first
-    constexpr int kPart = paged_part_floats<D, NG>();
+    constexpr int kPart = paged_part_floats<D, NG>();              // per set of heads: accumulators, then maxima and sums
     const int from = paged_share_owner(total, n_act, unit0 + kPagedItemUnits);
     const int to = paged_share_owner(total, n_act, unit0 + kPagedItemUnits + n_tiles - 1);
     // parts of a round of the join: half of the ring; `from`'s lies apart from the others
@@ -581,60 +562,48 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
       const int skip = q0 == 0 ? 1 : 0;
       if (n > skip) bulk_load(dst + skip * kPart * 4, a.part + (long long)(from + q0 + skip) * kPart, (uint32_t)(n - skip) * kPart * 4, bar_join(r & 1));
     };
-    if (warp == 0) {
-      float* dst = a.part + ((t0 == 0 ? (long long)gridDim.x : 0) + cta) * kPart;
+    const int acc_at = team * MT * 32 + lane, ml_at = NG * MT * 32 + team * 4 + c;   // in units of four floats
+    if (mate == 0) {
+      float4* dst = reinterpret_cast<float4*>(a.part + ((t0 == 0 ? (long long)gridDim.x : 0) + cta) * kPart);
 #pragma unroll
-      for (int i = 0; i < NG * MT; ++i) {
-        const float* v = o[i / MT][i % MT];
-        reinterpret_cast<float4*>(dst)[i * 32 + lane] = make_float4(v[0], v[1], v[2], v[3]);
-      }
-      if (g == 0) {
-#pragma unroll
-        for (int ng = 0; ng < NG; ++ng)
-          reinterpret_cast<float4*>(dst + NG * 8 * D)[ng * 4 + c] = make_float4(m[ng][0], m[ng][1], l[ng][0], l[ng][1]);
-      }
-      __syncwarp();
-      if (lane == 0) {
-        // the part is visible before the count goes up, and who counts last sees the others'
-        const int last = atom_add_acq_rel(a.tickets + item, 1) == to - from;
-        *s_last = last;
-        if (last) {
-          a.tickets[item] = 0;                                     // ready for the next call
-          if (!more) {
-            fence_proxy_async_global();                            // the parts are read by bulk copies, which
-            fence_proxy_async_smem();                              // overwrite tiles that all warps have done with
-            fetch(0);
-            fetch(1);
-          }
+      for (int mt = 0; mt < MT; ++mt) dst[acc_at + mt * 32] = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+      if (g == 0) dst[ml_at] = make_float4(m[0], m[1], l[0], l[1]);
+    }
+    if constexpr (NG == 1) __syncwarp(); else paged_consumers_sync();
+    if (tid == 0) {
+      // the part is visible before the count goes up, and who counts last sees the others'
+      const int last = atom_add_acq_rel(a.tickets + item, 1) == to - from;
+      *s_last = last;
+      if (last) {
+        a.tickets[item] = 0;                                       // ready for the next call
+        if (!more) {
+          fence_proxy_async_global();                              // the parts are read by bulk copies, which
+          fence_proxy_async_smem();                                // overwrite tiles that all warps have done with
+          fetch(0);
+          fetch(1);
         }
       }
     }
     paged_consumers_sync();
     if (*s_last) {
       clear();
-      auto join = [&](auto ml_of, auto v_of) {                     // adds one part
-        float f[NG][2], e[NG][2];
+      auto join = [&](const float4 ml, auto v_of) {                // adds one part
+        float f[2], e[2];
 #pragma unroll
-        for (int ng = 0; ng < NG; ++ng) {
-          const float4 ml = ml_of(ng);
-#pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const float top = x ? ml.y : ml.x, now = fmaxf(m[ng][x], top), ref = now == -INFINITY ? 0.f : now;
-            f[ng][x] = exp2f(m[ng][x] - ref);
-            e[ng][x] = exp2f(top - ref);
-            l[ng][x] = fmaf(x ? ml.w : ml.z, e[ng][x], l[ng][x] * f[ng][x]);
-            m[ng][x] = now;
-          }
+        for (int x = 0; x < 2; ++x) {
+          const float top = x ? ml.y : ml.x, now = fmaxf(m[x], top), ref = now == -INFINITY ? 0.f : now;
+          f[x] = exp2f(m[x] - ref);
+          e[x] = exp2f(top - ref);
+          l[x] = fmaf(x ? ml.w : ml.z, e[x], l[x] * f[x]);
+          m[x] = now;
         }
 #pragma unroll
-        for (int i = 0; i < NG * MT; ++i) {
-          const float4 v = v_of(i);
-          float* t = o[i / MT][i % MT];
-          const float *fn = f[i / MT], *en = e[i / MT];
-          t[0] = fmaf(v.x, en[0], t[0] * fn[0]);
-          t[1] = fmaf(v.y, en[1], t[1] * fn[1]);
-          t[2] = fmaf(v.z, en[0], t[2] * fn[0]);
-          t[3] = fmaf(v.w, en[1], t[3] * fn[1]);
+        for (int mt = 0; mt < MT; ++mt) {
+          const float4 v = v_of(mt);
+          o[mt][0] = fmaf(v.x, e[0], o[mt][0] * f[0]);
+          o[mt][1] = fmaf(v.y, e[1], o[mt][1] * f[1]);
+          o[mt][2] = fmaf(v.z, e[0], o[mt][2] * f[0]);
+          o[mt][3] = fmaf(v.w, e[1], o[mt][3] * f[1]);
         }
       };
       if (!more) {
@@ -645,9 +614,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
           if (!__all_sync(0xffffffffu, landed)) {
             if (lane == 0) record_status(p.status, kStatusTimeout);
           } else {
-            for (int q = warp; q < n; q += kPagedWarps) {
+            for (int q = mate; q < n; q += kTeam) {
               const float4* src = reinterpret_cast<const float4*>(gen + (r & 1) * kRound * kPart * 4) + q * (kPart / 4);
-              join([&](int ng) { return src[NG * 2 * D + ng * 4 + c]; }, [&](int i) { return src[i * 32 + lane]; });
+              join(src[ml_at], [&](int mt) { return src[acc_at + mt * 32]; });
             }
           }
           paged_consumers_sync();                                  // the half is read
@@ -657,13 +626,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
           }
         }
       } else {
-        for (int q = from + warp; q <= to; q += kPagedWarps) {
+        for (int q = from + mate; q <= to; q += kTeam) {
           const float4* src = reinterpret_cast<const float4*>(a.part + ((q == from ? (long long)gridDim.x : 0) + q) * kPart);
-          join([&](int ng) { return __ldcg(src + NG * 2 * D + ng * 4 + c); }, [&](int i) { return __ldcg(src + i * 32 + lane); });
+          join(__ldcg(src + ml_at), [&](int mt) { return __ldcg(src + acc_at + mt * 32); });
         }
       }
       merge_warps();
-      if (warp == 0) finish(b, head);
+      if (mate == 0) finish(b, head);
     }
     paged_consumers_sync();                                        // s_last is read
   }

@@ -40,11 +40,12 @@ struct PagedAppendArgs {
   int* tickets;                                            // [n_seqs] CTAs that have read the length; zero between calls
 };
 
-constexpr int kPagedAppendThreads = 256;
+constexpr int kPagedAppendThreads = 256, kPagedAppendCtas = 6;   // per SM
+constexpr int kPagedAppendRows = 2;                        // of a thread
 
 template <int VECS>
-__global__ void __launch_bounds__(kPagedAppendThreads, 4) paged_append_kernel(const PagedAppendArgs a) {
-  constexpr int kPer = kPagedAppendThreads / VECS, N = 4;  // rows side by side, rows of a thread
+__global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_append_kernel(const PagedAppendArgs a) {
+  constexpr int kPer = kPagedAppendThreads / VECS, N = kPagedAppendRows;
   allow_dependents();
   const PagedPool& p = a.pool;
   const int b = blockIdx.y, part = threadIdx.x % VECS;
@@ -58,33 +59,38 @@ __global__ void __launch_bounds__(kPagedAppendThreads, 4) paged_append_kernel(co
     count = 0;                                             // nothing of this sequence
   }
   const int n_rows = count * p.H, r0 = (int)blockIdx.x * (kPer * N) + threadIdx.x / VECS;   // below 2^31: the host looks
-  uint4 kv[N], vv[N];
-  long long to[N];
+  // Nothing is loaded under a condition, so that the rows of a thread are under way together; rows past the end repeat the last.
+  if (r0 < n_rows) {
+    uint4 kv[N], vv[N];
+    int page[N], at[N];
+    float w[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int r = r0 + j * kPer;
-    to[j] = -1;
-    if (r >= n_rows) continue;
-    const int i = r / p.H, h = r - i * p.H;
-    const int page = p.page(b, held + i), row = (held + i) & (p.page_size() - 1);
-    if ((unsigned)page >= (unsigned)p.n_pages) {           // never written outside the pool
-      if (part == 0) record_status(p.status, kPagedBadPage);
-      continue;
+    for (int j = 0; j < N; ++j) {
+      const int r = min(r0 + j * kPer, n_rows - 1), i = r / p.H, h = r - i * p.H;
+      page[j] = p.page(b, held + i);
+      kv[j] = ld_nc_v4(a.K + b * a.ks[0] + h * a.ks[1] + i * a.ks[2] + part * 8);
+      vv[j] = ld_nc_v4(a.V + b * a.vs[0] + h * a.vs[1] + i * a.vs[2] + part * 8);
+      at[j] = a.at ? a.at[b * a.as[0] + h * a.as[1] + i] : seen + i;
+      w[j] = a.w ? a.w[b * a.ws[0] + h * a.ws[1] + i] : 0.f;
     }
-    kv[j] = ld_nc_v4(a.K + b * a.ks[0] + h * a.ks[1] + i * a.ks[2] + part * 8);
-    vv[j] = ld_nc_v4(a.V + b * a.vs[0] + h * a.vs[1] + i * a.vs[2] + part * 8);
-    to[j] = page * a.rows.s_page + h * a.rows.s_head + row * a.rows.s_row;
-    if (part == 0) {
-      const long long slot = (((long long)page * p.H + h) << p.page_shift) + row;
-      a.rows.pos[slot] = a.at ? a.at[b * a.as[0] + h * a.as[1] + i] : seen + i;
-      if (a.rows.weights) a.rows.weights[slot] = a.w ? a.w[b * a.ws[0] + h * a.ws[1] + i] : 0.f;
-    }
-  }
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    if (to[j] < 0) continue;
-    *reinterpret_cast<uint4*>(a.rows.K + to[j] + part * 8) = kv[j];
-    *reinterpret_cast<uint4*>(a.rows.V + to[j] + part * 8) = vv[j];
+    for (int j = 0; j < N; ++j) {
+      if (r0 + j * kPer >= n_rows) continue;
+      const int r = r0 + j * kPer, i = r / p.H, h = r - i * p.H;
+      if ((unsigned)page[j] >= (unsigned)p.n_pages) {      // never written outside the pool
+        if (part == 0) record_status(p.status, kPagedBadPage);
+        continue;
+      }
+      const int row = (held + i) & (p.page_size() - 1);
+      const long long to = page[j] * a.rows.s_page + h * a.rows.s_head + row * a.rows.s_row + part * 8;
+      *reinterpret_cast<uint4*>(a.rows.K + to) = kv[j];
+      *reinterpret_cast<uint4*>(a.rows.V + to) = vv[j];
+      if (part == 0) {
+        const long long slot = (((long long)page[j] * p.H + h) << p.page_shift) + row;
+        a.rows.pos[slot] = at[j];
+        if (a.rows.weights) a.rows.weights[slot] = w[j];
+      }
+    }
   }
   __syncthreads();                                         // the whole CTA has read the length
   if (threadIdx.x == 0 && !bad) {
@@ -102,18 +108,19 @@ __global__ void __launch_bounds__(kPagedAppendThreads, 4) paged_append_kernel(co
 }
 
 // ------------------------------------------------------------------------------------------------
-// Eviction. One cluster per (sequence, KV head); every CTA holds the sort keys of a slice of the entries in shared memory.
+// Eviction. paged_evict_kernel: one cluster per (sequence, KV head); every CTA holds the sort keys of a slice of the entries in
+// shared memory.
 //   1. keys: the weight as an ordered integer, the largest for protected entries (the first positions and the last ones),
 //      -inf for NaN, which therefore leaves first.
 //   2. the keep-th largest key, by radix rounds over the eleven highest bits in which undecided keys can differ (as in
 //      take_topk), the histograms summed across the cluster; protected keys, often the most, are counted apart, so that they
-//      do not pile up in one bin.
+//      do not pile up in one bin. A lone CTA ranks the last few undecided keys against one another instead of further rounds.
 //   3. a sweep in index order with two counts (keys above, keys equal to it) gives every entry its rank among the kept ones.
 //      An evicted entry before `keep` is a hole, a kept one behind it a mover; holes are counted from the start, movers from the end,
-//      and the pairs go to a list.
-//   4. the cluster's warps move rows by the list. All sources lie behind `keep`, all destinations before it: no move
-//      waits for another, and only rows that have to move are touched. (Closing the gaps in order would move nearly every row.)
-// Reads 8 bytes per entry and moves two rows per hole: bound by HBM for large calls, by barriers and round trips for small ones.
+//      and the pairs go to a list, as slots of the pool.
+// paged_move_kernel moves rows by the lists, with all SMs, and sets the lengths. All sources lie behind `keep`, all destinations
+// before it: no move waits for another, and only rows that have to move are touched. (Closing the gaps in order would move
+// nearly every row.) The first kernel reads 8 bytes per entry and is bound by barriers and round trips, the second by HBM.
 // ------------------------------------------------------------------------------------------------
 struct PagedEvictArgs {
   PagedPool pool;
@@ -121,11 +128,12 @@ struct PagedEvictArgs {
   int keep, anchors, recent;
   int2* moves;                                             // lists of (hole, mover): per sequence, per KV head
   long long n_moves;                                       // pairs that `moves` holds
-  int* ticket;                                             // clusters that are done; zero between calls
+  int2* lists;                                             // [n_seqs][H] where each list starts and how long it is
 };
 
 constexpr int kEvictThreads = 512;
 constexpr int kEvictWarps = kEvictThreads / 32;
+constexpr int kEvictFew = 256;                             // undecided keys that a lone CTA ranks directly
 
 struct EvictShared {
   int hist[kSelBins];                                      // this CTA's; zero between rounds
@@ -136,16 +144,16 @@ struct EvictShared {
   uint32_t lo[kEvictWarps], hi[kEvictWarps];
   int prot[kEvictWarps];
   uint32_t range[2];                                       // smallest and largest unprotected key of the CTA
-  int n_prot;
+  int n_prot, n_few;
+  uint32_t few[kEvictFew];
   int above[kEvictWarps], equal[kEvictWarps], holes[kEvictWarps];
   int totals[3];                                           // CTA: keys above, keys equal, holes
-  int offset_lo;                                           // (sequence, head)'s place in the list
-  int last;
+  int offset;                                              // (sequence, head)'s place in the list
 };
 
 __host__ __device__ constexpr uint32_t evict_smem_bytes(int slice) { return (uint32_t)slice * 4u + (uint32_t)sizeof(EvictShared) + 16u; }
-// Entries of a CTA's slice: whole warps' worths.
-LKV_HOST_DEVICE inline int evict_slice(long long len, int n) { return (int)((len + n - 1) / n + kEvictThreads - 1) / kEvictThreads * kEvictThreads; }
+// Entries of a CTA's slice.
+LKV_HOST_DEVICE inline int evict_slice(long long len, int n) { return (int)((len + n - 1) / n + 31) / 32 * 32; }
 
 __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   uint32_t v;
@@ -164,55 +172,57 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   auto remote = [&](const void* at, int r) { return ld_cluster_u32(cluster_addr(smem_u32(at), r)); };
   for (int i = tid; i < kSelBins; i += kEvictThreads) sh.hist[i] = 0;
+  if (tid == 0) sh.n_few = 0;
+  // Lengths and page numbers are asked for one after the other: the L2 cache gets them together and ahead.
+  for (int i = tid * 32; i < p.max_pages; i += kEvictThreads * 32) prefetch_l2(p.table + (long long)b * p.max_pages + i);
+  if (tid < 2) prefetch_l2((tid ? p.seen : p.lens) + b);
   grid_dependency_wait();
   allow_dependents();
 
   const int len = p.length(b), keep = a.keep;
-  // Lengths change only when every cluster has read all that it needs of them: the last one does it.
-  auto done = [&]() {
-    if (rank == 0 && tid == 0) {
-      __threadfence();
-      const int all = (int)(gridDim.y * gridDim.z);
-      sh.last = atomicAdd(a.ticket, 1) == all - 1;
-      if (sh.last) *a.ticket = 0;
-    }
-    __syncthreads();
-    if (rank == 0 && sh.last)
-      for (int i = tid; i < p.n_seqs; i += kEvictThreads)
-        if (p.lens[i] > keep) p.lens[i] = keep;
-  };
-  if (len != p.lens[b] && tid == 0) record_status(p.status, kPagedBadPage);
+  const int held = p.lens[b], newest = p.seen[b] - a.recent;
+  if (warp == 1) {
+    // the place of this (sequence, head)'s pairs in the list: at most min(keep, len - keep) per head of the sequences before
+    long long pairs = 0;
+    for (int i = lane; i < b; i += 32) pairs += max(0, min(keep, p.length(i) - keep));
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) pairs += __shfl_xor_sync(0xffffffffu, pairs, off);
+    const long long most = max(0, min(keep, len - keep)), at = pairs * p.H + (long long)h * most;
+    // the list is as large as a pool whose pages are not shared can need
+    if (lane == 0) sh.offset = at + most <= a.n_moves ? (int)at : -1;
+  }
+  if (len != held && tid == 0) record_status(p.status, kPagedBadPage);
   if (len <= keep) {                                       // the same in all of the cluster
-    if (C > 1) cluster_sync(); else __syncthreads();       // all of it has read the length
-    done();
+    if (rank == 0 && tid == 0) a.lists[b * p.H + h] = make_int2(0, 0);
     return;
   }
 
   // ---- 1. keys ----------------------------------------------------------------------------------
   const int slice = evict_slice(len, C), lo_i = min(len, rank * slice), n = min(len - lo_i, slice);
-  const int newest = p.seen[b] - a.recent;
   uint32_t lo = 0xFFFFFFFFu, hi = 0u;
   int prot = 0;
-  for (int i0 = tid; i0 < n; i0 += 4 * kEvictThreads) {
-    int page[4], at[4];
-    float x[4];
+  constexpr int kAtOnce = 8;                               // keys of a thread under way together: nothing is loaded under a condition
+  for (int i0 = tid; i0 < n; i0 += kAtOnce * kEvictThreads) {
+    int page[kAtOnce], at[kAtOnce];
+    float x[kAtOnce];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) page[j] = i0 + j * kEvictThreads < n ? p.page(b, lo_i + i0 + j * kEvictThreads) : -1;
+    for (int j = 0; j < kAtOnce; ++j) page[j] = p.page(b, lo_i + min(i0 + j * kEvictThreads, n - 1));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int i = i0 + j * kEvictThreads;
+    for (int j = 0; j < kAtOnce; ++j) {
+      const int i = lo_i + min(i0 + j * kEvictThreads, n - 1);
       const bool ok = (unsigned)page[j] < (unsigned)p.n_pages;
-      const long long slot = (((long long)page[j] * p.H + h) << p.page_shift) + ((lo_i + i) & (p.page_size() - 1));
-      x[j] = ok ? a.rows.weights[slot] : -INFINITY;
-      at[j] = ok ? a.rows.pos[slot] : a.anchors;
-      if (i < n && !ok) record_status(p.status, kPagedBadPage);
+      const long long slot = (((long long)(ok ? page[j] : 0) * p.H + h) << p.page_shift) + (i & (p.page_size() - 1));
+      x[j] = a.rows.weights[slot];
+      at[j] = a.rows.pos[slot];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < kAtOnce; ++j) {
       const int i = i0 + j * kEvictThreads;
       if (i >= n) continue;
-      const bool safe = at[j] < a.anchors || at[j] >= newest || x[j] == INFINITY;
-      const uint32_t key = safe ? kEvictProtected : orderable_f32(x[j] != x[j] ? -INFINITY : x[j] + 0.f);   // + 0: -0 is 0
+      const bool bad = (unsigned)page[j] >= (unsigned)p.n_pages;     // counts as -inf
+      if (bad) record_status(p.status, kPagedBadPage);
+      const bool safe = !bad && (at[j] < a.anchors || at[j] >= newest || x[j] == INFINITY);
+      const uint32_t key = safe ? kEvictProtected : orderable_f32(bad || x[j] != x[j] ? -INFINITY : x[j] + 0.f);   // + 0: -0 is 0
       keys[i] = key;
       prot += safe;
       if (!safe) { lo = min(lo, key); hi = max(hi, key); }
@@ -223,14 +233,12 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
   prot = __reduce_add_sync(0xffffffffu, prot);
   if (lane == 0) { sh.lo[warp] = lo; sh.hi[warp] = hi; sh.prot[warp] = prot; }
   __syncthreads();
-  if (warp == 0) {
-    lo = __reduce_min_sync(0xffffffffu, sh.lo[lane % kEvictWarps]);
-    hi = __reduce_max_sync(0xffffffffu, sh.hi[lane % kEvictWarps]);
-    prot = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.prot[lane] : 0);
-    if (lane == 0) { sh.range[0] = lo; sh.range[1] = hi; sh.n_prot = prot; }
-  }
-  if (C > 1) cluster_sync(); else __syncthreads();
-  {
+  lo = __reduce_min_sync(0xffffffffu, sh.lo[lane % kEvictWarps]);
+  hi = __reduce_max_sync(0xffffffffu, sh.hi[lane % kEvictWarps]);
+  prot = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.prot[lane] : 0);
+  if (C > 1) {
+    if (tid == 0) { sh.range[0] = lo; sh.range[1] = hi; sh.n_prot = prot; }
+    cluster_sync();
     const int r = lane < C ? lane : 0;
     lo = __reduce_min_sync(0xffffffffu, remote(&sh.range[0], r));
     hi = __reduce_max_sync(0xffffffffu, remote(&sh.range[1], r));
@@ -240,12 +248,9 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
   // ---- 2. the keep-th largest key ----------------------------------------------------------------
   // kept: keys from `from` on, and of those equal to `tie` the first `ties` in index order
   uint32_t from = kEvictProtected, tie = kEvictProtected;
-  long long ties = 0;
-  bool with_ties = false;
+  int ties = 0;                                            // 0: none goes by its index
   if (prot >= keep) {
-    from = 0;                                              // none by being above
-    with_ties = true;
-    ties = keep;
+    ties = keep;                                           // of the protected ones themselves; none is above them
   } else {
     int need = keep - prot;                                // of len - prot > need unprotected ones
     uint32_t base = lo;
@@ -266,17 +271,22 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
         int mine = 0;
         for (int i = tid; i < per; i += kEvictThreads) {
           int v = 0;
-          for (int r = 0; r < C; ++r) v += (int)remote(&sh.hist[rank * per + i], r);
+          for (int r0 = 0; r0 < C; r0 += 4) {              // four reads under way together
+            int x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = (int)remote(&sh.hist[rank * per + i], min(r0 + r, C - 1));
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (r0 + r < C) v += x[r];
+          }
           sh.sums[i] = v;
           mine += v;
         }
         mine = __reduce_add_sync(0xffffffffu, mine);
         if (lane == 0) sh.chunk[warp] = mine;
         __syncthreads();
-        if (tid == 0) {
-          int s = 0;
-          for (int i = 0; i < kEvictWarps; ++i) s += sh.chunk[i];
-          sh.share = s;
+        if (warp == 0) {
+          const int s = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.chunk[lane] : 0);
+          if (lane == 0) sh.share = s;
         }
         cluster_sync();                                    // sums are written, histograms read
         // the share that holds the need-th from the top
@@ -322,9 +332,9 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
       __syncthreads();
       const uint32_t bin = (uint32_t)sh.found[0];
       need = sh.found[1];
-      const int held = sh.found[2];
+      const int held_in = sh.found[2];
       base += bin << shift;
-      if (need == held) {                                  // the whole bin
+      if (need == held_in) {                               // the whole bin
         from = base;
         break;
       }
@@ -332,37 +342,57 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
         from = base + 1;                                   // base < kEvictProtected
         tie = base;
         ties = need;
-        with_ties = true;
         break;
       }
       span_hi = (uint64_t)base + (1ull << shift) - 1;
+      if (C == 1 && held_in <= kEvictFew) {
+        for (int i0 = warp * 32; i0 < n; i0 += kEvictThreads) {
+          const int i = i0 + lane;
+          const uint32_t key = i < n ? keys[i] : kEvictProtected;
+          const bool in = key != kEvictProtected && key >= base && key <= span_hi;
+          const uint32_t mask = __ballot_sync(0xffffffffu, in);
+          int at = 0;
+          if (lane == 0 && mask) at = atomicAdd(&sh.n_few, __popc(mask));
+          at = __shfl_sync(0xffffffffu, at, 0) + __popc(mask & ((1u << lane) - 1u));
+          if (in) sh.few[at] = key;                        // in any order
+        }
+        __syncthreads();
+        if (tid < held_in) {
+          const uint32_t key = sh.few[tid];
+          int over = 0, same = 0;
+#pragma unroll 4
+          for (int i = 0; i < held_in; ++i) {
+            over += sh.few[i] > key;
+            same += sh.few[i] == key;
+          }
+          if (over < need && need <= over + same) {        // the threads that hold the need-th agree
+            sh.found[0] = (int)key;
+            sh.found[1] = need - over;
+          }
+        }
+        __syncthreads();
+        tie = (uint32_t)sh.found[0];
+        ties = sh.found[1];
+        from = tie + 1;
+        break;
+      }
       shift = shift > kSelBinBits ? shift - kSelBinBits : 0;
     }
   }
-  const bool none_above = with_ties && tie == kEvictProtected;
+  const bool any_above = tie != kEvictProtected || ties == 0;
 
   // ---- 3. ranks and the list of moves -------------------------------------------------------------
-  const int run_n = slice / kEvictWarps, w_lo = min(n, warp * run_n), w_hi = min(n, w_lo + run_n);
+  const int run_n = (slice / 32 + kEvictWarps - 1) / kEvictWarps * 32, w_lo = min(n, warp * run_n), w_hi = min(n, w_lo + run_n);
   {
     int above = 0, equal = 0;
     for (int i = w_lo + lane; i < w_hi; i += 32) {
       const uint32_t key = keys[i];
-      above += !none_above && key >= from;
-      equal += with_ties && key == tie;
+      above += any_above && key >= from;
+      equal += ties > 0 && key == tie;
     }
     above = __reduce_add_sync(0xffffffffu, above);
     equal = __reduce_add_sync(0xffffffffu, equal);
     if (lane == 0) { sh.above[warp] = above; sh.equal[warp] = equal; }
-  }
-  // the place of this (sequence, head)'s pairs: at most min(keep, len - keep) per head
-  if (warp == 1) {
-    long long sum = 0;
-    for (int i = lane; i < b; i += 32) sum += max(0, min(keep, p.length(i) - keep));
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    const long long most = min(keep, len - keep), at = sum * p.H + (long long)h * most;
-    // the list is as large as a pool whose pages are not shared can need
-    if (lane == 0) sh.offset_lo = at + most <= a.n_moves ? (int)at : -1;
   }
   __syncthreads();
   int above0 = 0, equal0 = 0;                              // before this warp's run
@@ -379,24 +409,27 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
       equal0 += __reduce_add_sync(0xffffffffu, re);
     }
   }
-  const bool room = sh.offset_lo >= 0;
-  int2* const list = a.moves + (room ? sh.offset_lo : 0);
+  const bool room = sh.offset >= 0;
+  int2* const list = a.moves + (room ? sh.offset : 0);
   int holes = 0;
   for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
     const int i = i0 + lane, e = lo_i + i;                 // entry
     const bool in = i < w_hi;
     const uint32_t key = in ? keys[i] : 0u;
-    const bool is_above = in && !none_above && key >= from, is_equal = in && with_ties && key == tie;
+    const bool is_above = in && any_above && key >= from, is_equal = in && ties > 0 && key == tie;
     const uint32_t ma = __ballot_sync(0xffffffffu, is_above), me = __ballot_sync(0xffffffffu, is_equal);
     const uint32_t below = (1u << lane) - 1u;
-    const long long eq = (long long)equal0 + __popc(me & below);
+    const int eq = equal0 + __popc(me & below);
     const bool kept = is_above || (is_equal && eq < ties);
-    const int kept_before = above0 + __popc(ma & below) + (int)(eq < ties ? eq : ties);
-    if (in && room) {
-      if (e < keep && !kept) list[e - kept_before].x = e;
-      if (e >= keep && kept) list[keep - 1 - kept_before].y = e;
+    const int kept_before = above0 + __popc(ma & below) + min(eq, ties);
+    const bool hole = in && e < keep && !kept, mover = in && e >= keep && kept;
+    if (room && (hole || mover)) {
+      const int page = p.page(b, e);                       // of a page out of range, recorded above: no slot
+      const int slot = (unsigned)page < (unsigned)p.n_pages ? (page << p.page_shift) + (e & (p.page_size() - 1)) : -1;
+      if (hole) list[e - kept_before].x = slot;
+      else list[keep - 1 - kept_before].y = slot;
     }
-    holes += in && e < keep && !kept;
+    holes += hole;
     above0 += __popc(ma);
     equal0 += __popc(me);
   }
@@ -407,52 +440,60 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
     holes = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.holes[lane] : 0);
     if (lane == 0) sh.totals[2] = holes;
   }
-  // ---- 4. moves ---------------------------------------------------------------------------------
-  if (C > 1) cluster_sync(); else __syncthreads();         // the list is written, by all of the cluster
-  const int total = __reduce_add_sync(0xffffffffu, lane < C ? (int)remote(&sh.totals[2], lane) : 0);
-  if (!room) {
-    if (tid == 0) record_status(p.status, kStatusCapacity);
-  } else {
-    const int vecs = a.rows.vecs, lanes = min(2 * vecs, 32), per_warp = 32 / lanes;   // lanes of a move: half on the key, half on the value
-    const int sub = lane / lanes, l = lane % lanes, half = lanes / 2;
-    const int step = C * kEvictWarps * per_warp;
-    constexpr int N = 4;                                   // moves of a thread under way together
-    for (int r0 = (rank * kEvictWarps + warp) * per_warp + sub; r0 < total; r0 += N * step) {
-      long long fr[N], to[N], sf[N], sd[N];
-      bool ok[N];
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const int r = r0 + j * step;
-        ok[j] = r < total;
-        const int2 mv = ok[j] ? __ldcg(list + r) : make_int2(0, 0);
-        const int pd = ok[j] ? p.page(b, mv.x) : -1, ps = ok[j] ? p.page(b, mv.y) : -1;
-        ok[j] = (unsigned)pd < (unsigned)p.n_pages && (unsigned)ps < (unsigned)p.n_pages;   // others were recorded above
-        const int rd = mv.x & (p.page_size() - 1), rs = mv.y & (p.page_size() - 1);
-        to[j] = pd * a.rows.s_page + h * a.rows.s_head + rd * a.rows.s_row;
-        fr[j] = ps * a.rows.s_page + h * a.rows.s_head + rs * a.rows.s_row;
-        sd[j] = (((long long)pd * p.H + h) << p.page_shift) + rd;
-        sf[j] = (((long long)ps * p.H + h) << p.page_shift) + rs;
-      }
-      uint16_t* const side = l < half ? a.rows.K : a.rows.V;
-      const int v0 = l < half ? l : l - half;
-      for (int v = v0; v < vecs; v += half) {
-        uint4 x[N];
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (ok[j]) x[j] = *reinterpret_cast<const uint4*>(side + fr[j] + v * 8);
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (ok[j]) *reinterpret_cast<uint4*>(side + to[j] + v * 8) = x[j];
-      }
-      if (l == 0) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (ok[j]) a.rows.weights[sd[j]] = a.rows.weights[sf[j]];
-      } else if (l == half) {
-#pragma unroll
-        for (int j = 0; j < N; ++j) if (ok[j]) a.rows.pos[sd[j]] = a.rows.pos[sf[j]];
-      }
-    }
+  if (C > 1) {
+    cluster_sync();
+    if (rank == 0 && warp == 0) holes = __reduce_add_sync(0xffffffffu, lane < C ? (int)remote(&sh.totals[2], lane) : 0);
+  }
+  if (rank == 0 && tid == 0) {
+    a.lists[b * p.H + h] = make_int2(sh.offset, room ? holes : 0);
+    if (!room) record_status(p.status, kStatusCapacity);
   }
   if (C > 1) cluster_sync();                               // no CTA leaves while another may read its shared memory
-  done();
+}
+
+constexpr int kMoveThreads = 256;
+
+// Moves the rows of the lists, one (sequence, KV head) per blockIdx (z, y), dealt to the warps of its gridDim.x CTAs.
+template <int VECS>
+__global__ void __launch_bounds__(kMoveThreads, 4) paged_move_kernel(const PagedEvictArgs a) {
+  constexpr int kLanes = VECS == 8 ? 16 : 32, kPerWarp = 32 / kLanes;   // lanes of a move: half on the key, half on the value
+  constexpr int kHalf = kLanes / 2, kTimes = VECS / kHalf, N = kTimes == 2 ? 2 : 4;   // 16-byte vectors of a lane; moves of a thread under way together
+  const PagedPool& p = a.pool;
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, l = lane % kLanes;
+  grid_dependency_wait();
+  allow_dependents();
+  if (blockIdx.x == 0 && h == 0 && tid == 0 && p.lens[b] > a.keep) p.lens[b] = a.keep;   // nothing else here goes by lengths
+  const int2 of = a.lists[b * p.H + h];
+  const int2* const list = a.moves + of.x;
+  uint16_t* const side = l < kHalf ? a.rows.K : a.rows.V;
+  int* const word = l < kHalf ? reinterpret_cast<int*>(a.rows.weights) : a.rows.pos;     // moved by lanes 0 and kHalf
+  const int v0 = (l % kHalf) * 8;
+  auto row = [&](int slot) {
+    return (slot >> p.page_shift) * a.rows.s_page + h * a.rows.s_head + (slot & (p.page_size() - 1)) * a.rows.s_row + v0;
+  };
+  auto entry = [&](int slot) { return (((long long)(slot >> p.page_shift) * p.H + h) << p.page_shift) + (slot & (p.page_size() - 1)); };
+  const int step = gridDim.x * (kMoveThreads / 32) * kPerWarp;
+  for (int r0 = (blockIdx.x * (kMoveThreads / 32) + (tid >> 5)) * kPerWarp + lane / kLanes; r0 < of.y; r0 += N * step) {
+    int2 mv[N];
+    uint4 x[N][kTimes];
+    int y[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) mv[j] = __ldcg(list + min(r0 + j * step, of.y - 1));
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int from = max(mv[j].y, 0);
+#pragma unroll
+      for (int k = 0; k < kTimes; ++k) x[j][k] = *reinterpret_cast<const uint4*>(side + row(from) + k * kHalf * 8);
+      y[j] = word[entry(from)];
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if (r0 + j * step >= of.y || mv[j].x < 0 || mv[j].y < 0) continue;
+#pragma unroll
+      for (int k = 0; k < kTimes; ++k) *reinterpret_cast<uint4*>(side + row(mv[j].x) + k * kHalf * 8) = x[j][k];
+      if (l % kHalf == 0) word[entry(mv[j].x)] = y[j];
+    }
+  }
 }
 
 }  // namespace lkv

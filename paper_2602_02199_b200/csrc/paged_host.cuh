@@ -16,6 +16,7 @@ struct laser_kv_paged_ctx {
   float* scores = nullptr;
   int2* score_at = nullptr;
   int2* moves = nullptr;
+  int2* lists = nullptr;
   int group, head_blocks, n_wide;           // query heads per KV head; blocks of 8 * n_wide of them
   int score_heads = 0;                      // scores of an entry
   int score_tiles = 0;
@@ -31,7 +32,7 @@ constexpr int paged_max_ctas(int d) { return d == 64 ? 480 : d == 128 ? 320 : 16
 struct PagedDerived {
   int group, n_wide, head_blocks, page_shift, score_tiles, score_heads;
   long long cap, n_moves;
-  size_t append_tickets, attn_tickets, part, lse2, scores, score_at, moves, zeroed, total;
+  size_t append_tickets, attn_tickets, part, lse2, scores, score_at, moves, lists, zeroed, total;
 };
 
 laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d) {
@@ -51,7 +52,7 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
   d->cap = (long long)c->max_pages * c->page_size;
   const long long rows = (long long)c->n_pages * c->page_size * c->n_kv_heads;
   d->group = c->n_q_heads / c->n_kv_heads;
-  d->n_wide = c->head_dim == 256 || d->group <= 8 ? 1 : 2;
+  d->n_wide = d->group <= 8 ? 1 : 2;
   d->head_blocks = (d->group + 8 * d->n_wide - 1) / (8 * d->n_wide);
   const long long seq_tiles = (d->cap + kDecTile - 1) / kDecTile + kPagedItemUnits;
   if (c->n_seqs > 65535 || c->n_kv_heads > 65535 || d->cap > (1ll << 30) || rows > 0x7fffffffLL ||
@@ -70,7 +71,7 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
     return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: weights for at most 128 query heads per KV head");
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes); return o; };
-  take(256);                                                   // status word, ticket of the eviction, units of the last accumulating call
+  take(256);                                                   // status word, units of the last accumulating call
   d->append_tickets = take((size_t)c->n_seqs * 4);
   d->attn_tickets = take((size_t)c->n_seqs * c->n_kv_heads * d->head_blocks * 4);
   d->zeroed = off;
@@ -79,6 +80,7 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
   d->scores = take((size_t)d->score_tiles * kDecTile * d->score_heads * sizeof(float));
   d->score_at = take((size_t)d->score_tiles * sizeof(int2));
   d->moves = take((size_t)d->n_moves * sizeof(int2));
+  d->lists = take(c->track_weights ? (size_t)c->n_seqs * c->n_kv_heads * sizeof(int2) : 0);
   d->total = off;
   return LASER_KV_OK;
 }
@@ -103,7 +105,9 @@ bool paged_map(EncodeTiledFn enc, CUtensorMap* m, const laser_kv_paged_config_t&
   const cuuint64_t bytes[3] = {(cuuint64_t)strides[2] * 2, (cuuint64_t)strides[1] * 2, (cuuint64_t)strides[0] * 2};
   const cuuint32_t box[4] = {64, (cuuint32_t)(c.page_size < kDecTile ? c.page_size : kDecTile), 1, 1}, ones[4] = {1, 1, 1, 1};
   return enc(m, c.dtype == LASER_KV_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(ptr), dims,
-             bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             bytes, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+             // rows of 128 bytes that lie apart: no more than a row is fetched, what is beside it belongs to another head
+             c.head_dim == 64 && strides[2] != 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -116,10 +120,8 @@ laser_kv_status_t paged_device(laser_kv_paged_ctx* h, const char* who) {
   return LASER_KV_OK;
 }
 
-cudaError_t evict_limits(int slice) {
-  // the limit grows with the largest slice asked for: the attribute is set for the largest there is
+cudaError_t evict_limits() {                  // set for the largest slice there is
   static std::atomic<unsigned long long> limit_set{0};
-  (void)slice;
   return ensure_smem_limit(limit_set, paged_evict_kernel, (int)evict_smem_bytes(kEvictKeys), true);
 }
 
@@ -136,7 +138,7 @@ bool evict_cluster_fits(int n, long long cap) {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int room = 0;
-  if (evict_limits(0) != cudaSuccess || cudaOccupancyMaxActiveClusters(&room, paged_evict_kernel, &cfg) != cudaSuccess) {
+  if (evict_limits() != cudaSuccess || cudaOccupancyMaxActiveClusters(&room, paged_evict_kernel, &cfg) != cudaSuccess) {
     cudaGetLastError();
     return false;
   }
@@ -159,13 +161,13 @@ cudaError_t launch_paged_attn_t(const laser_kv_paged_ctx* h, const PagedAttnArgs
   switch (h->cfg.head_dim) {
     case 64: return h->n_wide == 1 ? launch_paged_attn<HALF, 64, 1>(h, a, st) : launch_paged_attn<HALF, 64, 2>(h, a, st);
     case 128: return h->n_wide == 1 ? launch_paged_attn<HALF, 128, 1>(h, a, st) : launch_paged_attn<HALF, 128, 2>(h, a, st);
-    default: return launch_paged_attn<HALF, 256, 1>(h, a, st);
+    default: return h->n_wide == 1 ? launch_paged_attn<HALF, 256, 1>(h, a, st) : launch_paged_attn<HALF, 256, 2>(h, a, st);
   }
 }
 
 template <int VECS>
 cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st) {
-  constexpr long long kRows = kPagedAppendThreads / VECS * 4;
+  constexpr long long kRows = kPagedAppendThreads / VECS * kPagedAppendRows;
   const long long rows = (long long)a.n_new * a.pool.H;
   return launch(paged_append_kernel<VECS>, dim3((unsigned)((rows + kRows - 1) / kRows), (unsigned)a.pool.n_seqs), kPagedAppendThreads, 0, st, true, a);
 }
@@ -240,6 +242,7 @@ laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* 
     h->scores = reinterpret_cast<float*>(ws + d.scores);
     h->score_at = reinterpret_cast<int2*>(ws + d.score_at);
     h->moves = reinterpret_cast<int2*>(ws + d.moves);
+    h->lists = reinterpret_cast<int2*>(ws + d.lists);
   }
   h->group = d.group;
   h->head_blocks = d.head_blocks;
@@ -341,7 +344,7 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
     a.lse2 = h->lse2;
     a.scores = h->scores;
     a.score_at = h->score_at;
-    a.score_units = reinterpret_cast<int*>(h->ws) + 2;
+    a.score_units = reinterpret_cast<int*>(h->ws) + 1;
     a.score_tiles = h->score_tiles;
     a.weights = h->rows.weights;
   }
@@ -367,13 +370,20 @@ laser_kv_status_t laser_kv_paged_evict(laser_kv_paged_handle_t h, int32_t keep, 
   if (keep >= h->cap) return LASER_KV_OK;
   if (!h->evict_ctas)
     return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged_evict: a table of %lld entries is longer than a cluster's shared memory sorts", h->cap);
-  cudaError_t e = evict_limits(0);
-  if (e == cudaSuccess) {
-    PagedEvictArgs a{h->pool, h->rows, keep, anchors, recent, h->moves, h->n_moves, reinterpret_cast<int*>(h->ws) + 1};
-    e = launch_clusters(paged_evict_kernel, dim3((unsigned)h->evict_ctas, (unsigned)h->cfg.n_kv_heads, (unsigned)h->cfg.n_seqs), kEvictThreads,
-                        evict_smem_bytes(evict_slice(h->cap, h->evict_ctas)), static_cast<cudaStream_t>(stream), true, h->evict_ctas, a);
-  }
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const PagedEvictArgs a{h->pool, h->rows, keep, anchors, recent, h->moves, h->n_moves, h->lists};
+  const int heads = h->cfg.n_kv_heads, seqs = h->cfg.n_seqs;
+  cudaError_t e = evict_limits();
+  if (e == cudaSuccess)
+    e = launch_clusters(paged_evict_kernel, dim3((unsigned)h->evict_ctas, (unsigned)heads, (unsigned)seqs), kEvictThreads,
+                        evict_smem_bytes(evict_slice(h->cap, h->evict_ctas)), st, true, h->evict_ctas, a);
   if (e != cudaSuccess) return fail(nullptr, LASER_KV_ERR_CUDA, "paged_evict_kernel launch: %s", cudaGetErrorString(e));
+  const unsigned ctas = (unsigned)move_ctas(h->num_sms, (long long)seqs * heads, keep < h->cap - keep ? keep : h->cap - keep);
+  const dim3 grid(ctas, (unsigned)heads, (unsigned)seqs);
+  e = h->rows.vecs == 8    ? launch(paged_move_kernel<8>, grid, kMoveThreads, 0, st, true, a)
+      : h->rows.vecs == 16 ? launch(paged_move_kernel<16>, grid, kMoveThreads, 0, st, true, a)
+                           : launch(paged_move_kernel<32>, grid, kMoveThreads, 0, st, true, a);
+  if (e != cudaSuccess) return fail(nullptr, LASER_KV_ERR_CUDA, "paged_move_kernel launch: %s", cudaGetErrorString(e));
   return LASER_KV_OK;
 }
 

@@ -46,7 +46,7 @@ def test_workspace_sizes(group, track, d):
     size = Bn.laser_kv_paged_query_sizes(cfg)
     assert size % 256 == 0
     # parts of the CTAs, and with weights a score per query head (a power of two of them) and entry, a pair of indices per two
-    wide, ctas = 1 if d == 256 or group <= 8 else 2, {64: 480, 128: 320, 256: 160}[d]
+    wide, ctas = 1 if group <= 8 else 2, {64: 480, 128: 320, 256: 160}[d]
     least = ctas * 2 * wide * 8 * (d + 2) * 4
     if track:
         heads = max(4, 1 << (group - 1).bit_length())
@@ -137,7 +137,9 @@ int main() {
         need((n == 0) == (cap > 49152ll * most), "limit", heads, cap);
         if (!n) continue;
         need(n <= most && (n & (n - 1)) == 0 && (long long)n * kEvictKeys >= cap, "cluster", heads, cap);
-        need(n == 1 || n * heads <= 148 || (long long)n / 2 * kEvictKeys < cap, "more than the SMs", heads, cap);
+        need(n == 1 || n * heads <= 296 || (long long)n / 2 * kEvictKeys < cap, "more than the SMs", heads, cap);
+        const int m = move_ctas(148, heads, cap);
+        need(m >= 1 && (m == 1 || (m * heads <= 8 * 148 && (m - 1) * 32ll < cap)), "movers", heads, cap);
       }
   return 0;
 }
