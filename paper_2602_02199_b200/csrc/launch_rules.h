@@ -126,25 +126,39 @@ LKV_HOST_DEVICE inline long long weighted_begin(long long part, int c, int n, co
 }
 
 // Paged cache. The items (a sequence and a KV head) are one list of units, kPagedItemUnits for each item and one for each of its
-// tiles, that is cut into equal contiguous shares, one per CTA (or warp): share c of n is [paged_share_begin(c),
-// paged_share_begin(c + 1)); with n <= total none is empty.
+// tiles, that is cut into equal contiguous shares, one per CTA: share c is [begin(c), begin(c + 1)), and none is empty.
+// (Divisions of 64 bits took a CTA 0.3 us to find its share.)
 constexpr int kPagedItemUnits = 2;
-LKV_HOST_DEVICE inline int paged_share_begin(int total, int n, int c) { return (int)((long long)total * c / n); }
-// The share that holds unit t.
-LKV_HOST_DEVICE inline int paged_share_owner(int total, int n, int t) { return (int)((((long long)t + 1) * n - 1) / total); }
-// Shares of an attention call on `grid` CTAs: of two units at least.
-LKV_HOST_DEVICE inline int paged_shares(int total, int grid) {
-  const int n = total - total / 2;
-  return n < grid ? n : grid;
-}
+struct PagedShares {
+  int total, n, each, rest;                // units, shares of two units at least, total = each * n + rest
+  LKV_HOST_DEVICE PagedShares(int units, int grid) : total(units) {
+    n = total - total / 2;
+    if (n > grid) n = grid;
+    each = n ? total / n : 0;
+    rest = total - each * n;
+  }
+  LKV_HOST_DEVICE int begin(int c) const { return each * c + rest * c / n; }     // total * c / n
+  // The share that holds unit t: an estimate that is off by one at most, put right.
+  LKV_HOST_DEVICE int owner(int t) const {
+    int c = (int)((float)t * ((float)n / (float)total));
+    if (c > n - 1) c = n - 1;
+    while (begin(c) > t) --c;
+    while (begin(c + 1) <= t) ++c;
+    return c;
+  }
+};
 
-// CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: at most kEvictKeys each (their sort keys stay in
-// shared memory), kEvictOwn where the SMs have room for two CTAs each. 0: more entries than `most` CTAs hold.
+// CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: kEvictOwn entries each while the device holds
+// all the call's clusters at once, at most kEvictKeys (their sort keys stay in shared memory). `room(n)`: how many clusters of n
+// the device holds at once, of sixteen seven on a B200. 0: more entries than the largest cluster holds. us for append and eviction of a block of
+// 4096 at a budget of 8192, 8 heads: clusters of one 39, of two 37, of four 31 (512 threads a CTA); at 32768 of eight 39, of
+// sixteen that take turns 62.
 constexpr int kEvictKeys = 49152, kEvictOwn = 4096;
-inline int evict_cluster(int num_sms, long long heads, long long cap, int most) {
+template <typename Room>
+inline int evict_cluster(long long heads, long long cap, Room&& room) {
   int n = 1;
-  while (n < most && 2 * n * heads <= 2ll * num_sms && cap > (long long)kEvictOwn * n) n *= 2;
-  while (n < most && cap > (long long)kEvictKeys * n) n *= 2;
+  while (n < 16 && cap > (long long)kEvictOwn * n && room(2 * n, cap) >= heads) n *= 2;
+  while (n < 16 && cap > (long long)kEvictKeys * n && room(2 * n, cap) > 0) n *= 2;
   return cap > (long long)kEvictKeys * n ? 0 : n;
 }
 

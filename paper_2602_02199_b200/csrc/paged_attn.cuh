@@ -15,9 +15,9 @@
 //   paged_weights_kernel  exp(x_i - lse) from the scores that the first kernel left (4 bytes per query head and entry
 //                         against the 512 of its key and value), added to the entries' weights.
 //
-// Numerators are taken relative to the maximum of their own 16 rows, where they are at most 1, and the 16 rows' sums are
+// Numerators are taken relative to the maximum of their own 16 (or 32) rows, where they are at most 1, and the rows' sums are
 // added to the running ones in fp32, rounded to nearest, with the factor between the two maxima. The MMAs' accumulators do not
-// round to nearest: over the 16 rows of a block that does not matter, over thousands it would be a drift. bf16: a numerator
+// round to nearest: over the few rows of a block that does not matter, over thousands it would be a drift. bf16: a numerator
 // is split into three terms, which hold all 24 bits. fp16: two terms of the numerator times 2^15 hold 22 bits down to
 // 2^-18 of the block's largest, 2^-40 of it below that.
 #pragma once
@@ -84,15 +84,20 @@ __host__ __device__ constexpr uint32_t paged_smem_bytes() {
   return 1024u + paged_stages<D>() * paged_stage_bytes<D>() + 2u * D / 16 * 512u + 2u * kPagedWarps * 8u * 4u + (2u * paged_stages<D>() + 2u) * 8u + 16u;
 }
 
-// D (16x8, fp32) += A (16x16, row) * B (16x8, col)
+// D (16x8, fp32) += A (16x16, row) * B (16x8, col). Not volatile: the compiler may interleave independent ones.
 template <bool HALF>
 __device__ __forceinline__ void paged_mma(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   if constexpr (HALF)
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    mma_bf16(d, a, b0, b1);
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t paged_trans(uint32_t x) {       // as movmatrix_trans
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 template <bool HALF>
 __device__ __forceinline__ uint32_t paged_pack(float lo, float hi) {
@@ -140,13 +145,6 @@ struct PagedWalk {
 
 __device__ __forceinline__ int paged_units(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile + kPagedItemUnits : 0; }
 
-// Units per item over all sequences; called by whole warps. `mine`: this lane's part, see paged_seek.
-__device__ __forceinline__ int paged_total(const PagedPool& p, int lane, int& mine) {
-  const int per = (p.n_seqs + 31) / 32;
-  mine = 0;
-  for (int i = lane * per; i < min((lane + 1) * per, p.n_seqs); ++i) mine += paged_units(p.length(i));
-  return __reduce_add_sync(0xffffffffu, mine);
-}
 __device__ __forceinline__ int warp_inclusive(int x, int lane) {
 #pragma unroll
   for (int off = 1; off < 32; off <<= 1) {
@@ -155,28 +153,44 @@ __device__ __forceinline__ int warp_inclusive(int x, int lane) {
   }
   return x;
 }
-// The place of unit `at` (below total * heads) of the list.
-__device__ __forceinline__ PagedWalk paged_seek(const PagedPool& p, int lane, int mine, int heads, int at) {
-  const int per = (p.n_seqs + 31) / 32, q = at / heads;    // the sequence: the first with more than q units per item up to its end
-  int incl = warp_inclusive(mine, lane);
-  const int who = (__ffs(__ballot_sync(0xffffffffu, incl > q)) - 1) & 31;
-  PagedWalk w;
-  w.before = __shfl_sync(0xffffffffu, incl - mine, who);
-  w.b = who * per;
-  for (;;) {
-    const int i = w.b + lane;
-    const int len = i < p.n_seqs ? p.length(i) : 0, u = paged_units(len);
-    incl = w.before + warp_inclusive(u, lane);
-    const uint32_t found = __ballot_sync(0xffffffffu, incl > q);
-    if (found || w.b + 32 >= p.n_seqs) {                   // `at` is in the list: found
-      const int l = (__ffs(found) - 1) & 31;
-      w.b += l;
-      w.before = __shfl_sync(0xffffffffu, incl - u, l);
-      w.len = max(1, __shfl_sync(0xffffffffu, len, l));
-      break;
+// Units per item over all sequences, and up to and with this lane's; called by whole warps. A lane has `per` sequences in a row.
+struct PagedSum {
+  int per, incl, mine, total, len;                         // len: the lane's only sequence's, where per is 1
+  __device__ __forceinline__ PagedSum(const PagedPool& p, int lane) {
+    per = (p.n_seqs + 31) >> 5;
+    mine = len = 0;
+    for (int i = lane * per; i < min((lane + 1) * per, p.n_seqs); ++i) {
+      len = p.length(i);
+      mine += paged_units(len);
     }
-    w.before = __shfl_sync(0xffffffffu, incl, 31);
-    w.b += 32;
+    incl = warp_inclusive(mine, lane);
+    total = __shfl_sync(0xffffffffu, incl, 31);
+  }
+};
+// The place of unit `at` (below total * heads) of the list.
+__device__ __forceinline__ PagedWalk paged_seek(const PagedPool& p, int lane, const PagedSum& sum, int heads, int at) {
+  const int q = at / heads;                                // the sequence: the first with more than q units per item up to its end
+  const int who = (__ffs(__ballot_sync(0xffffffffu, sum.incl > q)) - 1) & 31;
+  PagedWalk w;
+  w.before = __shfl_sync(0xffffffffu, sum.incl - sum.mine, who);
+  w.b = who * sum.per;
+  w.len = __shfl_sync(0xffffffffu, sum.len, who);
+  if (sum.per > 1) {
+    for (;;) {
+      const int i = w.b + lane;
+      const int len = i < p.n_seqs ? p.length(i) : 0, u = paged_units(len);
+      const int incl = w.before + warp_inclusive(u, lane);
+      const uint32_t found = __ballot_sync(0xffffffffu, incl > q);
+      if (found || w.b + 32 >= p.n_seqs) {                 // `at` is in the list: found
+        const int l = (__ffs(found) - 1) & 31;
+        w.b += l;
+        w.before = __shfl_sync(0xffffffffu, incl - u, l);
+        w.len = __shfl_sync(0xffffffffu, len, l);
+        break;
+      }
+      w.before = __shfl_sync(0xffffffffu, incl, 31);
+      w.b += 32;
+    }
   }
   w.n_tiles = (w.len + kDecTile - 1) / kDecTile;
   w.head = (at - w.before * heads) / w.units();
@@ -246,16 +260,14 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   grid_dependency_wait();
   allow_dependents();
 
-  int mine;
-  const int total = paged_total(p, lane, mine) * heads;
-  const int n_act = paged_shares(total, (int)gridDim.x);
+  const PagedSum sum(p, lane);
+  const PagedShares shares(sum.total * heads, (int)gridDim.x);
   const int cta = blockIdx.x;
-  const int begin = cta < n_act ? paged_share_begin(total, n_act, cta) : 0;
-  const int stop = cta < n_act ? paged_share_begin(total, n_act, cta + 1) : 0;
+  const int begin = cta < shares.n ? shares.begin(cta) : 0, stop = cta < shares.n ? shares.begin(cta + 1) : 0;
   bool more = begin < stop;
   PagedWalk w{};
-  if (more) w = paged_seek(p, lane, mine, heads, begin);
-  if (a.scores && cta == 0 && tid == 0) *a.score_units = total / a.head_blocks;
+  if (more) w = paged_seek(p, lane, sum, heads, begin);
+  if (a.scores && cta == 0 && tid == 0) *a.score_units = sum.total * p.H;
 
   if (warp == kPagedWarps) {
     // ---- producer ---------------------------------------------------------------------------------
@@ -307,8 +319,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   }
 
   // ---- consumers ------------------------------------------------------------------------------------
-  // With one set of eight heads a warp has 16 rows of every tile; with two, a pair of warps has a set, a warp of it 32 rows, 16
-  // at a time: a warp's registers hold eight heads either way.
+  // With one set of eight heads a warp has 16 rows of every tile; with two, a pair of warps has a set, a warp of it 32 rows: a
+  // warp's registers hold eight heads either way.
   constexpr int kTeam = kPagedWarps / NG;                          // warps of a set
   const int g = lane >> 2, c = lane & 3;                           // fragment coordinates, as in decode_split_kernel
   const int team = warp / kTeam, mate = warp % kTeam;
@@ -448,39 +460,45 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         if (lane == 0) record_status(p.status, kStatusTimeout);
         gone = true;
       }
-#pragma unroll
-      for (int blk = 0; blk < NG; ++blk) {                         // 16 rows
-        const int row0 = mate * (16 * NG) + 16 * blk, rows = w.len - t * kDecTile - row0;   // rows that the sequence has from row0 on
-        if (gone || rows <= 0) continue;
+      const int row0 = mate * (16 * NG), rows = w.len - t * kDecTile - row0;   // the warp's first row, how many the sequence has from there on
+      if (!gone && rows > 0) {
         const uint32_t k_tile = base + st * paged_stage_bytes<D>(), v_tile = k_tile + kHalf;
-        float x[4] = {0.f, 0.f, 0.f, 0.f}, x1[4] = {0.f, 0.f, 0.f, 0.f};   // two chains
+        float x[NG][4];                                            // scores, then numerators, of 16 rows each
 #pragma unroll
-        for (int ks = 0; ks < MT; ks += 2) {
-          uint32_t k0[4], k1[4];
-          ldsm_x4(k_tile + dec_swz(row0 + (lane & 15), 2 * ks + (lane >> 4)), k0);
-          ldsm_x4(k_tile + dec_swz(row0 + (lane & 15), 2 * ks + 2 + (lane >> 4)), k1);
-          paged_mma<HALF>(x, k0, qb[ks][0], qb[ks][1]);
-          paged_mma<HALF>(x1, k1, qb[ks + 1][0], qb[ks + 1][1]);
+        for (int r = 0; r < NG; ++r) {
+          float x1[4] = {0.f, 0.f, 0.f, 0.f};                      // two chains
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[r][i] = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < MT; ks += 2) {
+            uint32_t k0[4], k1[4];
+            ldsm_x4(k_tile + dec_swz(row0 + 16 * r + (lane & 15), 2 * ks + (lane >> 4)), k0);
+            ldsm_x4(k_tile + dec_swz(row0 + 16 * r + (lane & 15), 2 * ks + 2 + (lane >> 4)), k1);
+            paged_mma<HALF>(x[r], k0, qb[ks][0], qb[ks][1]);
+            paged_mma<HALF>(x1, k1, qb[ks + 1][0], qb[ks + 1][1]);
+          }
+          // rows past the sequence's end hold whatever the page or an earlier tile left there
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[r][i] = 16 * r + g + (i & 2) * 4 < rows ? (x[r][i] + x1[i]) * a.scale_log2e : -INFINITY;
         }
-        // rows past the sequence's end hold whatever the page or an earlier tile left there
-        const bool v_lo = g < rows, v_hi = g + 8 < rows;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (i < 2 ? v_lo : v_hi) ? (x[i] + x1[i]) * a.scale_log2e : -INFINITY;
         const int unit = score_unit + kPagedItemUnits + t;
         if (a.scores && unit < a.score_tiles) {
           const int hg = first_head(w.head, h) + 2 * c;
-          if (tid == 0 && blk == 0) a.score_at[unit] = make_int2((int)((unsigned)w.b | (unsigned)h << 16), t);
+          if (tid == 0) a.score_at[unit] = make_int2((int)((unsigned)w.b | (unsigned)h << 16), t);
           float* dst = a.scores + ((long long)unit * kDecTile + row0 + g) * a.Gs + hg;
           if (hg < a.G) {
-            if (v_lo) *reinterpret_cast<float2*>(dst) = make_float2(x[0], x[1]);
-            if (v_hi) *reinterpret_cast<float2*>(dst + 8 * a.Gs) = make_float2(x[2], x[3]);
+#pragma unroll
+            for (int r = 0; r < 2 * NG; ++r)
+              if (8 * r + g < rows) *reinterpret_cast<float2*>(dst + 8 * r * a.Gs) = make_float2(x[r / 2][2 * (r & 1)], x[r / 2][2 * (r & 1) + 1]);
           }
         }
         float alpha[2], beta[2];
         bool raise = false;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
-          float top = fmaxf(x[y], x[y + 2]);
+          float top = fmaxf(x[0][y], x[0][y + 2]);
+#pragma unroll
+          for (int r = 1; r < NG; ++r) top = fmaxf(top, fmaxf(x[r][y], x[r][y + 2]));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
           const float ref = top == -INFINITY ? 0.f : top;
@@ -489,42 +507,53 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
           beta[y] = exp2f(top - run);
           raise |= now > old;
           m[y] = now;
-          x[y] = exp2f(x[y] - ref);
-          x[y + 2] = exp2f(x[y + 2] - ref);
-          l[y] = fmaf(x[y] + x[y + 2], beta[y], l[y] * alpha[y]);
-          if constexpr (HALF) {                                    // exact: powers of two
-            x[y] *= 32768.f;
-            x[y + 2] *= 32768.f;
-            beta[y] *= 1.f / 32768.f;
-          }
-        }
-        uint32_t pb[HALF ? 2 : 3][2];                              // B fragments of P^T, term by term
+          float part = 0.f;
 #pragma unroll
-        for (int term = 0; term < (HALF ? 2 : 3); ++term) {
-          const uint32_t lo = paged_pack<HALF>(x[0], x[1]), hi = paged_pack<HALF>(x[2], x[3]);
-          pb[term][0] = movmatrix_trans(lo);
-          pb[term][1] = movmatrix_trans(hi);
-          const float2 f0 = paged_unpack<HALF>(lo), f1 = paged_unpack<HALF>(hi);
-          x[0] -= f0.x; x[1] -= f0.y; x[2] -= f1.x; x[3] -= f1.y;
+          for (int r = 0; r < NG; ++r) {
+            x[r][y] = exp2f(x[r][y] - ref);
+            x[r][y + 2] = exp2f(x[r][y + 2] - ref);
+            part += x[r][y] + x[r][y + 2];
+            if constexpr (HALF) {                                  // exact: powers of two
+              x[r][y] *= 32768.f;
+              x[r][y + 2] *= 32768.f;
+            }
+          }
+          l[y] = fmaf(part, beta[y], l[y] * alpha[y]);
+          if constexpr (HALF) beta[y] *= 1.f / 32768.f;
         }
+        constexpr int kTerms = HALF ? 2 : 3;
+        uint32_t pb[NG][kTerms][2];                                // B fragments of P^T, term by term
+#pragma unroll
+        for (int r = 0; r < NG; ++r)
+#pragma unroll
+          for (int term = 0; term < kTerms; ++term) {
+            const uint32_t lo = paged_pack<HALF>(x[r][0], x[r][1]), hi = paged_pack<HALF>(x[r][2], x[r][3]);
+            pb[r][term][0] = paged_trans(lo);
+            pb[r][term][1] = paged_trans(hi);
+            const float2 f0 = paged_unpack<HALF>(lo), f1 = paged_unpack<HALF>(hi);
+            x[r][0] -= f0.x; x[r][1] -= f0.y; x[r][2] -= f1.x; x[r][3] -= f1.y;
+          }
         if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[mt][i] *= alpha[i & 1];
         }
-        if (rows < 16) {                                           // values of rows past the end: 0 times what lies there could be NaN
-          for (int i = rows * (D / 8) + lane; i < 16 * (D / 8); i += 32) st_shared_zero(v_tile + dec_swz(row0 + i / (D / 8), i % (D / 8)));
+        if (rows < 16 * NG) {                                      // values of rows past the end: 0 times what lies there could be NaN
+          for (int i = rows * (D / 8) + lane; i < 16 * NG * (D / 8); i += 32) st_shared_zero(v_tile + dec_swz(row0 + i / (D / 8), i % (D / 8)));
           fence_proxy_async_smem();                                // before a later tile is brought here
           __syncwarp();
         }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
-          uint32_t vt[4];
-          ldsm_x4_trans(v_tile + dec_swz(row0 + (lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), vt);
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int term = 0; term < (HALF ? 2 : 3); ++term) paged_mma<HALF>(sum, vt, pb[term][0], pb[term][1]);
+          for (int r = 0; r < NG; ++r) {
+            uint32_t vt[4];
+            ldsm_x4_trans(v_tile + dec_swz(row0 + 16 * r + (lane & 7) + 8 * (lane >> 4), 2 * mt + ((lane >> 3) & 1)), vt);
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term) paged_mma<HALF>(sum, vt, pb[r][term][0], pb[r][term][1]);
+          }
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[mt][i] = fmaf(sum[i], beta[i & 1], o[mt][i]);
         }
@@ -549,8 +578,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     }
     // the item's parts lie in consecutive CTAs: its start in the first one's second slot, the others in their first
     constexpr int kPart = paged_part_floats<D, NG>();              // per set of heads: accumulators, then maxima and sums
-    const int from = paged_share_owner(total, n_act, unit0 + kPagedItemUnits);
-    const int to = paged_share_owner(total, n_act, unit0 + kPagedItemUnits + n_tiles - 1);
+    const int from = shares.owner(unit0 + kPagedItemUnits), to = shares.owner(unit0 + kPagedItemUnits + n_tiles - 1);
     // parts of a round of the join: half of the ring; `from`'s lies apart from the others
     constexpr int kRound = kStages * paged_stage_bytes<D>() / 2 / (kPart * 4);
     auto fetch = [&](int r) {                                      // one thread: round r, if there is one

@@ -131,7 +131,7 @@ struct PagedEvictArgs {
   int2* lists;                                             // [n_seqs][H] where each list starts and how long it is
 };
 
-constexpr int kEvictThreads = 512;
+constexpr int kEvictThreads = 1024;
 constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictFew = 256;                             // undecided keys that a lone CTA ranks directly
 
@@ -146,8 +146,8 @@ struct EvictShared {
   uint32_t range[2];                                       // smallest and largest unprotected key of the CTA
   int n_prot, n_few;
   uint32_t few[kEvictFew];
-  int above[kEvictWarps], equal[kEvictWarps], holes[kEvictWarps];
-  int totals[3];                                           // CTA: keys above, keys equal, holes
+  int above[kEvictWarps], equal[kEvictWarps];
+  int totals[2];                                           // CTA: keys above, keys equal
   int offset;                                              // (sequence, head)'s place in the list
 };
 
@@ -161,9 +161,12 @@ __device__ __forceinline__ uint32_t ld_cluster_u32(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
-__global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const PagedEvictArgs a) {
+__global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const PagedEvictArgs a) {
   extern __shared__ __align__(16) uint8_t esm_raw[];
   EvictShared& sh = *reinterpret_cast<EvictShared*>(esm_raw);
   uint32_t* const keys = reinterpret_cast<uint32_t*>(esm_raw + (sizeof(EvictShared) + 15) / 16 * 16);
@@ -173,9 +176,6 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
   auto remote = [&](const void* at, int r) { return ld_cluster_u32(cluster_addr(smem_u32(at), r)); };
   for (int i = tid; i < kSelBins; i += kEvictThreads) sh.hist[i] = 0;
   if (tid == 0) sh.n_few = 0;
-  // Lengths and page numbers are asked for one after the other: the L2 cache gets them together and ahead.
-  for (int i = tid * 32; i < p.max_pages; i += kEvictThreads * 32) prefetch_l2(p.table + (long long)b * p.max_pages + i);
-  if (tid < 2) prefetch_l2((tid ? p.seen : p.lens) + b);
   grid_dependency_wait();
   allow_dependents();
 
@@ -201,7 +201,7 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
   const int slice = evict_slice(len, C), lo_i = min(len, rank * slice), n = min(len - lo_i, slice);
   uint32_t lo = 0xFFFFFFFFu, hi = 0u;
   int prot = 0;
-  constexpr int kAtOnce = 8;                               // keys of a thread under way together: nothing is loaded under a condition
+  constexpr int kAtOnce = 4;                               // keys of a thread under way together: nothing is loaded under a condition
   for (int i0 = tid; i0 < n; i0 += kAtOnce * kEvictThreads) {
     int page[kAtOnce], at[kAtOnce];
     float x[kAtOnce];
@@ -407,11 +407,11 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
       const int ra = lane < rank ? (int)remote(&sh.totals[0], lane) : 0, re = lane < rank ? (int)remote(&sh.totals[1], lane) : 0;
       above0 += __reduce_add_sync(0xffffffffu, ra);
       equal0 += __reduce_add_sync(0xffffffffu, re);
+      cluster_arrive();                                    // the last look at another CTA's shared memory
     }
   }
   const bool room = sh.offset >= 0;
   int2* const list = a.moves + (room ? sh.offset : 0);
-  int holes = 0;
   for (int i0 = w_lo; i0 < w_hi; i0 += 32) {
     const int i = i0 + lane, e = lo_i + i;                 // entry
     const bool in = i < w_hi;
@@ -429,26 +429,15 @@ __global__ void __launch_bounds__(kEvictThreads, 2) paged_evict_kernel(const Pag
       if (hole) list[e - kept_before].x = slot;
       else list[keep - 1 - kept_before].y = slot;
     }
-    holes += hole;
+    if (in && e == keep) {                                 // entry `keep` knows how many holes are before it
+      a.lists[b * p.H + h] = make_int2(sh.offset, room ? keep - kept_before : 0);
+      if (!room) record_status(p.status, kStatusCapacity);
+    }
     above0 += __popc(ma);
     equal0 += __popc(me);
   }
-  holes = __reduce_add_sync(0xffffffffu, holes);
-  if (lane == 0) sh.holes[warp] = holes;
-  __syncthreads();
-  if (warp == 0) {
-    holes = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.holes[lane] : 0);
-    if (lane == 0) sh.totals[2] = holes;
-  }
-  if (C > 1) {
-    cluster_sync();
-    if (rank == 0 && warp == 0) holes = __reduce_add_sync(0xffffffffu, lane < C ? (int)remote(&sh.totals[2], lane) : 0);
-  }
-  if (rank == 0 && tid == 0) {
-    a.lists[b * p.H + h] = make_int2(sh.offset, room ? holes : 0);
-    if (!room) record_status(p.status, kStatusCapacity);
-  }
-  if (C > 1) cluster_sync();                               // no CTA leaves while another may read its shared memory
+  __syncwarp();
+  if (C > 1) cluster_wait();                               // no CTA leaves while another may read its shared memory
 }
 
 constexpr int kMoveThreads = 256;

@@ -125,8 +125,9 @@ cudaError_t evict_limits() {                  // set for the largest slice there
   return ensure_smem_limit(limit_set, paged_evict_kernel, (int)evict_smem_bytes(kEvictKeys), true);
 }
 
-// Whether the current device holds a cluster of n eviction CTAs.
-bool evict_cluster_fits(int n, long long cap) {
+// How many clusters of n eviction CTAs, of a slice of `cap` entries each, the current device holds at once; 0 also where it cannot say.
+int evict_room(int n, long long cap) {
+  if (cap > (long long)kEvictKeys * n) return 1;      // a slice that no CTA has: asked for on the way to a larger cluster
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(n);
   cfg.blockDim = dim3(kEvictThreads);
@@ -140,9 +141,9 @@ bool evict_cluster_fits(int n, long long cap) {
   int room = 0;
   if (evict_limits() != cudaSuccess || cudaOccupancyMaxActiveClusters(&room, paged_evict_kernel, &cfg) != cudaSuccess) {
     cudaGetLastError();
-    return false;
+    return 0;
   }
-  return room > 0;
+  return room;
 }
 
 template <bool HALF, int D, int NG>
@@ -264,8 +265,7 @@ laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* 
   }
   if (weights) {
     const long long heads = (long long)cfg->n_seqs * cfg->n_kv_heads;
-    h->evict_ctas = evict_cluster(sms, heads, d.cap, 16);
-    if (h->evict_ctas > 8 && !evict_cluster_fits(h->evict_ctas, d.cap)) h->evict_ctas = evict_cluster(sms, heads, d.cap, 8);
+    h->evict_ctas = evict_cluster(heads, d.cap, evict_room);
   }
   *out = h;
   return LASER_KV_OK;

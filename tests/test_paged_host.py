@@ -119,25 +119,28 @@ static void need(bool ok, const char* what, long long a, long long b) { if (!ok)
 int main() {
   const int totals[] = {1, 2, 3, 7, 147, 148, 149, 295, 296, 297, 1000, 4097, 123457, 2147483647};
   for (int total : totals)
-    for (int grid : {1, 2, 3, 148, 296, 320}) {
-      const int n = paged_shares(total, grid);
+    for (int grid : {1, 2, 3, 148, 296, 444, 480}) {
+      const PagedShares s(total, grid);
+      const int n = s.n;
       need(n >= 1 && n <= grid && n <= total, "shares", total, grid);
-      need(paged_share_begin(total, n, 0) == 0 && paged_share_begin(total, n, n) == total, "ends", total, n);
+      need(s.begin(0) == 0 && s.begin(n) == total, "ends", total, n);
       for (int c = 0; c < n; ++c) {
-        const int lo = paged_share_begin(total, n, c), hi = paged_share_begin(total, n, c + 1);
-        need(hi > lo, "empty share", total, c);
-        need(paged_share_owner(total, n, lo) == c && paged_share_owner(total, n, hi - 1) == c && paged_share_owner(total, n, lo + (hi - lo) / 2) == c, "owner", total, c);
+        const int lo = s.begin(c), hi = s.begin(c + 1);
+        need(lo == (long long)total * c / n && hi > lo, "empty share", total, c);
+        need(s.owner(lo) == c && s.owner(hi - 1) == c && s.owner(lo + (hi - lo) / 2) == c, "owner", total, c);
       }
     }
-  need(paged_shares(0, 296) == 0, "no tiles", 0, 0);
+  need(PagedShares(0, 296).n == 0, "no tiles", 0, 0);
   for (long long heads : {1ll, 2ll, 8ll, 30ll, 64ll, 100ll, 512ll, 100000ll})
     for (long long cap : {8ll, 64ll, 1024ll, 1025ll, 2056ll, 40960ll, 49152ll, 49153ll, 400000ll, 786432ll, 786433ll})
       for (int most : {8, 16}) {
-        const int n = evict_cluster(148, heads, cap, most);
+        // a device of 148 SMs with a CTA each, in parts of 18
+        auto room = [most](int n, long long) { return n > most ? 0 : 8 * (18 / n); };
+        const int n = evict_cluster(heads, cap, room);
         need((n == 0) == (cap > 49152ll * most), "limit", heads, cap);
         if (!n) continue;
         need(n <= most && (n & (n - 1)) == 0 && (long long)n * kEvictKeys >= cap, "cluster", heads, cap);
-        need(n == 1 || n * heads <= 296 || (long long)n / 2 * kEvictKeys < cap, "more than the SMs", heads, cap);
+        need(n == 1 || room(n, cap) >= heads || (long long)n / 2 * kEvictKeys < cap, "more than the device holds", heads, cap);
         const int m = move_ctas(148, heads, cap);
         need(m >= 1 && (m == 1 || (m * heads <= 8 * 148 && (m - 1) * 32ll < cap)), "movers", heads, cap);
       }
