@@ -35,6 +35,7 @@ namespace lkv {
 
 constexpr int kPagedWarps = 4;                             // consumer warps, 16 rows of every tile each
 constexpr int kPagedThreads = (kPagedWarps + 1) * 32;
+constexpr float kPagedLeast = -3.4e38f;                    // stands for a maximum of -inf where it is subtracted: all powers are 0
 constexpr int kPagedBadPage = 1;                           // status of a page number or length out of range: LASER_KV_ERR_INVALID_ARG
 
 struct PagedPool {                                         // what all kernels of a paged cache are told about it
@@ -153,15 +154,26 @@ __device__ __forceinline__ int warp_inclusive(int x, int lane) {
   }
   return x;
 }
-// Units per item over all sequences, and up to and with this lane's; called by whole warps. A lane has `per` sequences in a row.
+// Units per item over all sequences, and up to and with this lane's; called by whole warps. A lane has `per` sequences in a row: one,
+// or, of more than 32, as many blocks of 32 as it takes.
 struct PagedSum {
   int per, incl, mine, total, len;                         // len: the lane's only sequence's, where per is 1
   __device__ __forceinline__ PagedSum(const PagedPool& p, int lane) {
-    per = (p.n_seqs + 31) >> 5;
-    mine = len = 0;
-    for (int i = lane * per; i < min((lane + 1) * per, p.n_seqs); ++i) {
-      len = p.length(i);
-      mine += paged_units(len);
+    if (p.n_seqs <= 32) {
+      per = 1;
+      len = lane < p.n_seqs ? p.length(lane) : 0;
+      mine = paged_units(len);
+    } else {
+      const int blocks = (p.n_seqs + 1023) >> 10;          // of a lane
+      per = 32 * blocks;
+      mine = len = 0;
+      const int n = (p.n_seqs + 31) >> 5;
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const int i = min(32 * k + lane, p.n_seqs - 1), u = paged_units(p.length(i));
+        const int s = __reduce_add_sync(0xffffffffu, 32 * k + lane < p.n_seqs ? u : 0);
+        if (k / blocks == lane) mine += s;
+      }
     }
     incl = warp_inclusive(mine, lane);
     total = __shfl_sync(0xffffffffu, incl, 31);
@@ -381,10 +393,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int wi = 0; wi < kTeam; ++wi) top = fmaxf(top, wm[wi * 8 + at]);
-      const float ref = top == -INFINITY ? 0.f : top;              // nothing above -inf: all factors are 0
+      const float ref = fmaxf(top, kPagedLeast);
 #pragma unroll
-      for (int wi = 0; wi < kTeam; ++wi) sum = fmaf(wl[wi * 8 + at], exp2f(wm[wi * 8 + at] - ref), sum);
-      const float f = exp2f(m[x] - ref);
+      for (int wi = 0; wi < kTeam; ++wi) sum = fmaf(wl[wi * 8 + at], ex2_approx(wm[wi * 8 + at] - ref), sum);
+      const float f = ex2_approx(m[x] - ref);
       m[x] = top;
       l[x] = sum;
 #pragma unroll
@@ -501,17 +513,16 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
           for (int r = 1; r < NG; ++r) top = fmaxf(top, fmaxf(x[r][y], x[r][y + 2]));
 #pragma unroll
           for (int off = 4; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-          const float ref = top == -INFINITY ? 0.f : top;
-          const float old = m[y], now = fmaxf(old, top), run = now == -INFINITY ? 0.f : now;
-          alpha[y] = exp2f(old - run);
-          beta[y] = exp2f(top - run);
+          const float ref = fmaxf(top, kPagedLeast), old = m[y], now = fmaxf(old, top), run = fmaxf(now, kPagedLeast);
+          alpha[y] = ex2_approx(old - run);
+          beta[y] = ex2_approx(top - run);
           raise |= now > old;
           m[y] = now;
           float part = 0.f;
 #pragma unroll
           for (int r = 0; r < NG; ++r) {
-            x[r][y] = exp2f(x[r][y] - ref);
-            x[r][y + 2] = exp2f(x[r][y + 2] - ref);
+            x[r][y] = ex2_approx(x[r][y] - ref);
+            x[r][y + 2] = ex2_approx(x[r][y + 2] - ref);
             part += x[r][y] + x[r][y + 2];
             if constexpr (HALF) {                                  // exact: powers of two
               x[r][y] *= 32768.f;
@@ -619,9 +630,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         float f[2], e[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const float top = x ? ml.y : ml.x, now = fmaxf(m[x], top), ref = now == -INFINITY ? 0.f : now;
-          f[x] = exp2f(m[x] - ref);
-          e[x] = exp2f(top - ref);
+          const float top = x ? ml.y : ml.x, now = fmaxf(m[x], top), ref = fmaxf(now, kPagedLeast);
+          f[x] = ex2_approx(m[x] - ref);
+          e[x] = ex2_approx(top - ref);
           l[x] = fmaf(x ? ml.w : ml.z, e[x], l[x] * f[x]);
           m[x] = now;
         }

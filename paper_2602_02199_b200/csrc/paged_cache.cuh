@@ -249,8 +249,9 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
   // kept: keys from `from` on, and of those equal to `tie` the first `ties` in index order
   uint32_t from = kEvictProtected, tie = kEvictProtected;
   int ties = 0;                                            // 0: none goes by its index
-  if (prot >= keep) {
-    ties = keep;                                           // of the protected ones themselves; none is above them
+  const bool any_above = prot < keep;
+  if (!any_above) {
+    ties = keep;                                           // of the protected ones themselves
   } else {
     int need = keep - prot;                                // of len - prot > need unprotected ones
     uint32_t base = lo;
@@ -379,7 +380,6 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
       shift = shift > kSelBinBits ? shift - kSelBinBits : 0;
     }
   }
-  const bool any_above = tie != kEvictProtected || ties == 0;
 
   // ---- 3. ranks and the list of moves -------------------------------------------------------------
   const int run_n = (slice / 32 + kEvictWarps - 1) / kEvictWarps * 32, w_lo = min(n, warp * run_n), w_hi = min(n, w_lo + run_n);

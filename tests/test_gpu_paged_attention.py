@@ -37,7 +37,7 @@ def test_attention_against_64_bits(dtype, D, G, H, page_size, token_major, lens)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
-@pytest.mark.parametrize("n", [33, 70, 1100])
+@pytest.mark.parametrize("n", [31, 32, 33, 70, 1023, 1024, 1025, 2500])
 def test_many_sequences(dtype, n):
     lens = [(i * 37) % 190 if i % 5 else 0 for i in range(n)]
     cache, gen = build(lens, H=2, G=2, D=64, page_size=16, dtype=dtype)

@@ -50,6 +50,8 @@ def test_ties_and_special_weights(values):
         cache.weights.copy_(torch.tensor(values, dtype=torch.float32, device="cuda")[pick])
         _evict(cache, keep, 5, 20)
         _evict(cache, keep // 2, 0, 0)
+        _evict(cache, 1, 0, 0)
+        _evict(cache, 0, 0, 0)
 
 
 @pytest.mark.parametrize("lens,H", [([60000], 1), ([60000, 30000], 8), ([400000], 2)])
