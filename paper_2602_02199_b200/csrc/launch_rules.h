@@ -162,9 +162,29 @@ inline int evict_cluster(long long heads, long long cap, Room&& room) {
   return cap > (long long)kEvictKeys * n ? 0 : n;
 }
 
-// CTAs that move the rows of one (sequence, KV head), of at most `moves`: 32 rows each, up to eight CTAs per SM in all.
+// Quotients of numbers below 2^31 by a fixed d of 1 to 65536, by a multiplication: with 2^s < d <= 2^(s + 1) and m = ceil(2^(32 + s) / d),
+// r * m / 2^(32 + s) exceeds r / d by less than r * d / (d * 2^(32 + s)) < 2^-(1 + s) <= 1 / d, which leaves the floor as it is.
+struct Quotient {
+  unsigned m, s, one;                      // one: d is 1
+  explicit Quotient(unsigned d = 1) : m(0), s(0), one(d == 1) {
+    if (one) return;
+    while ((2ull << s) < d) ++s;
+    m = (unsigned)(((1ull << (32 + s)) + d - 1) / d);
+  }
+  LKV_HOST_DEVICE int of(int r) const { return one ? r : (int)(((unsigned long long)(unsigned)r * m >> 32) >> s); }
+};
+
+// How often a CTA of an append takes its rows, `per` at a time, of each sequence's `rows` at most: once while that leaves a dozen
+// CTAs per SM or fewer, up to kAppendTimes times in large calls, where CTAs behind the end of a short sequence cost a start each.
+constexpr int kAppendTimes = 4;
+inline int append_times(int num_sms, long long n_seqs, long long rows, int per) {
+  const long long ctas = (rows + per - 1) / per * n_seqs, n = ctas / (12ll * num_sms);
+  return n < 1 ? 1 : n < kAppendTimes ? (int)n : kAppendTimes;
+}
+
+// CTAs that move the rows of one (sequence, KV head), of at most `moves`: 32 rows each, up to four CTAs per SM in all.
 inline int move_ctas(int num_sms, long long heads, long long moves) {
-  const long long n = (moves + 31) / 32, room = 8ll * num_sms / heads;
+  const long long n = (moves + 31) / 32, room = 4ll * num_sms / heads;
   return (int)(n < room ? (n > 0 ? n : 1) : room > 0 ? room : 1);
 }
 

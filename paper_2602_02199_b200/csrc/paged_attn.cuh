@@ -287,7 +287,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     const int per_shift = 6 - rows_shift;                          // pages of a tile
     const uint64_t once = l2_evict_first();
     int st = 0, round = 0;
-    for (; more; more = w.next(p, heads, stop)) {
+    for (bool ok = true; ok && more; more = w.next(p, heads, stop)) {
       const int first = w.first(begin), end = w.last(stop), h = w.head / a.head_blocks;
       const int last_page = (w.len - 1) >> p.page_shift;
       int ids = 0;
@@ -305,7 +305,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         const int id = __shfl_sync(0xffffffffu, ids, (k << per_shift) + (lane & ((1 << per_shift) - 1)));
         if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_empty(st), (uint32_t)(round - 1) & 1u))) {
           if (lane == 0) record_status(p.status, kStatusTimeout);
-          return;                                                  // the consumers' waits run out, too
+          ok = false;                                              // the consumers' waits run out, too
+          break;
         }
         if (lane == 0) mbar_expect_tx(bar_full(st), (uint32_t)pages << (rows_shift + 7 + (D == 64 ? 1 : D == 128 ? 2 : 3)));
         __syncwarp();
@@ -327,6 +328,8 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         if (++st == kStages) { st = 0; ++round; }
       }
     }
+    // no tile is still on its way here when the CTA ends, also where a consumer has given up
+    for (int n = round * kStages + st - 1, k = 0; n >= 0 && k < kStages; --n, ++k) mbar_wait(bar_full(n % kStages), (uint32_t)(n / kStages) & 1u);
     return;
   }
 

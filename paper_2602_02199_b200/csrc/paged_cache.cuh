@@ -22,9 +22,9 @@ struct PagedRows {                                         // where the rows of 
 };
 
 // ------------------------------------------------------------------------------------------------
-// Append. Rows (token, head) of a sequence, head by head within a token, are dealt to CTAs of kPagedAppendRows; a thread has a
-// vector of the key and of the value of up to four rows under way. Bound by HBM for prompts, by round trips (length, page,
-// row) for single tokens. The last CTA of a sequence to have read its length advances it.
+// Append. Rows (token, head) of a sequence, head by head within a token, are dealt to CTAs; a thread has a vector of the key and of
+// the value of two rows under way, several times over. Bound by HBM for prompts, by round trips (length, page, row) for
+// single tokens. The last CTA of a sequence to have read its length advances it.
 // ------------------------------------------------------------------------------------------------
 struct PagedAppendArgs {
   PagedPool pool;
@@ -36,16 +36,17 @@ struct PagedAppendArgs {
   const int* at;                                           // their positions or NULL (counted on)
   long long ws[2], as[2];                                  // strides: sequence, head
   const int* counts;                                       // [n_seqs] or NULL (n_new)
-  int n_new;
+  int n_new, times;                                        // entries at most; how often a CTA takes kPagedAppendRows rows per thread
+  Quotient by_heads;                                       // rows of a token
   int* tickets;                                            // [n_seqs] CTAs that have read the length; zero between calls
 };
 
-constexpr int kPagedAppendThreads = 256, kPagedAppendCtas = 6;   // per SM
+constexpr int kPagedAppendThreads = 256, kPagedAppendCtas = 5;   // per SM
 constexpr int kPagedAppendRows = 2;                        // of a thread
 
 template <int VECS>
 __global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_append_kernel(const PagedAppendArgs a) {
-  constexpr int kPer = kPagedAppendThreads / VECS, N = kPagedAppendRows;
+  constexpr int kPer = kPagedAppendThreads / VECS, N = kPagedAppendRows;   // rows side by side; of a thread
   allow_dependents();
   const PagedPool& p = a.pool;
   const int b = blockIdx.y, part = threadIdx.x % VECS;
@@ -58,39 +59,41 @@ __global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_a
     if (threadIdx.x == 0) record_status(p.status, bad);
     count = 0;                                             // nothing of this sequence
   }
-  const int n_rows = count * p.H, r0 = (int)blockIdx.x * (kPer * N) + threadIdx.x / VECS;   // below 2^31: the host looks
+  const int n_rows = count * p.H, first = (int)blockIdx.x * (kPer * N * a.times), last = min(n_rows, first + kPer * N * a.times);   // below 2^31: the host looks
   // Nothing is loaded under a condition, so that the rows of a thread are under way together; rows past the end repeat the last.
-  if (r0 < n_rows) {
+  const uint16_t *src_k = a.K + b * a.ks[0] + part * 8, *src_v = a.V + b * a.vs[0] + part * 8;
+  for (int r0 = first + threadIdx.x / VECS; r0 < last; r0 += kPer * N) {
     uint4 kv[N], vv[N];
-    int page[N], at[N];
-    float w[N];
+    int page[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int r = min(r0 + j * kPer, n_rows - 1), i = r / p.H, h = r - i * p.H;
+      const int r = min(r0 + j * kPer, n_rows - 1), i = a.by_heads.of(r), h = r - i * p.H;
       page[j] = p.page(b, held + i);
-      kv[j] = ld_nc_v4(a.K + b * a.ks[0] + h * a.ks[1] + i * a.ks[2] + part * 8);
-      vv[j] = ld_nc_v4(a.V + b * a.vs[0] + h * a.vs[1] + i * a.vs[2] + part * 8);
-      at[j] = a.at ? a.at[b * a.as[0] + h * a.as[1] + i] : seen + i;
-      w[j] = a.w ? a.w[b * a.ws[0] + h * a.ws[1] + i] : 0.f;
+      kv[j] = ld_nc_v4(src_k + h * a.ks[1] + i * a.ks[2]);
+      vv[j] = ld_nc_v4(src_v + h * a.vs[1] + i * a.vs[2]);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      if (r0 + j * kPer >= n_rows) continue;
-      const int r = r0 + j * kPer, i = r / p.H, h = r - i * p.H;
+      const int r = r0 + j * kPer, i = a.by_heads.of(r), h = r - i * p.H;
+      if (r >= n_rows) continue;
       if ((unsigned)page[j] >= (unsigned)p.n_pages) {      // never written outside the pool
         if (part == 0) record_status(p.status, kPagedBadPage);
         continue;
       }
-      const int row = (held + i) & (p.page_size() - 1);
-      const long long to = page[j] * a.rows.s_page + h * a.rows.s_head + row * a.rows.s_row + part * 8;
+      const long long to = page[j] * a.rows.s_page + h * a.rows.s_head + ((held + i) & (p.page_size() - 1)) * a.rows.s_row + part * 8;
       *reinterpret_cast<uint4*>(a.rows.K + to) = kv[j];
       *reinterpret_cast<uint4*>(a.rows.V + to) = vv[j];
-      if (part == 0) {
-        const long long slot = (((long long)page[j] * p.H + h) << p.page_shift) + row;
-        a.rows.pos[slot] = at[j];
-        if (a.rows.weights) a.rows.weights[slot] = w[j];
-      }
     }
+  }
+  // positions and weights, a row per thread
+  for (int r = first + threadIdx.x; r < last; r += kPagedAppendThreads) {
+    const int i = a.by_heads.of(r), h = r - i * p.H, page = p.page(b, held + i);
+    const int at = a.at ? a.at[b * a.as[0] + h * a.as[1] + i] : seen + i;
+    const float w = a.w ? a.w[b * a.ws[0] + h * a.ws[1] + i] : 0.f;
+    if ((unsigned)page >= (unsigned)p.n_pages) continue;
+    const long long slot = (((long long)page * p.H + h) << p.page_shift) + ((held + i) & (p.page_size() - 1));
+    a.rows.pos[slot] = at;
+    if (a.rows.weights) a.rows.weights[slot] = w;
   }
   __syncthreads();                                         // the whole CTA has read the length
   if (threadIdx.x == 0 && !bad) {

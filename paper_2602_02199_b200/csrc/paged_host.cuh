@@ -167,10 +167,12 @@ cudaError_t launch_paged_attn_t(const laser_kv_paged_ctx* h, const PagedAttnArgs
 }
 
 template <int VECS>
-cudaError_t launch_paged_append(const PagedAppendArgs& a, cudaStream_t st) {
-  constexpr long long kRows = kPagedAppendThreads / VECS * kPagedAppendRows;
+cudaError_t launch_paged_append(PagedAppendArgs a, int num_sms, cudaStream_t st) {
   const long long rows = (long long)a.n_new * a.pool.H;
-  return launch(paged_append_kernel<VECS>, dim3((unsigned)((rows + kRows - 1) / kRows), (unsigned)a.pool.n_seqs), kPagedAppendThreads, 0, st, true, a);
+  a.by_heads = Quotient((unsigned)a.pool.H);
+  a.times = append_times(num_sms, a.pool.n_seqs, rows, kPagedAppendThreads / VECS * kPagedAppendRows);
+  const long long per = (long long)kPagedAppendThreads / VECS * kPagedAppendRows * a.times;
+  return launch(paged_append_kernel<VECS>, dim3((unsigned)((rows + per - 1) / per), (unsigned)a.pool.n_seqs), kPagedAppendThreads, 0, st, true, a);
 }
 
 }  // namespace
@@ -309,7 +311,8 @@ laser_kv_status_t laser_kv_paged_append(laser_kv_paged_handle_t h, const void* K
   a.n_new = n_new;
   a.tickets = h->append_tickets;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = h->rows.vecs == 8 ? launch_paged_append<8>(a, st) : h->rows.vecs == 16 ? launch_paged_append<16>(a, st) : launch_paged_append<32>(a, st);
+  const cudaError_t e = h->rows.vecs == 8 ? launch_paged_append<8>(a, h->num_sms, st)
+                        : h->rows.vecs == 16 ? launch_paged_append<16>(a, h->num_sms, st) : launch_paged_append<32>(a, h->num_sms, st);
   if (e != cudaSuccess) return fail(nullptr, LASER_KV_ERR_CUDA, "paged_append_kernel launch: %s", cudaGetErrorString(e));
   return LASER_KV_OK;
 }

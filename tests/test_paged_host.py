@@ -142,8 +142,16 @@ int main() {
         need(n <= most && (n & (n - 1)) == 0 && (long long)n * kEvictKeys >= cap, "cluster", heads, cap);
         need(n == 1 || room(n, cap) >= heads || (long long)n / 2 * kEvictKeys < cap, "more than the device holds", heads, cap);
         const int m = move_ctas(148, heads, cap);
-        need(m >= 1 && (m == 1 || (m * heads <= 8 * 148 && (m - 1) * 32ll < cap)), "movers", heads, cap);
+        need(m >= 1 && (m == 1 || (m * heads <= 4 * 148 && (m - 1) * 32ll < cap)), "movers", heads, cap);
       }
+  for (unsigned d = 1; d <= 65536; d = d < 300 ? d + 1 : d * 5 / 4) {
+    const Quotient q(d);
+    for (long long r : {0ll, 1ll, (long long)d - 1, (long long)d, 2ll * d - 1, 12345ll, 1000003ll, (1ll << 30) / d * d - 1, (1ll << 30) / d * d, 2147483647ll / d * d - 1,
+                        2147483647ll / d * d, 2147483647ll, 2147483646ll})
+      if (r >= 0 && r <= 2147483647ll) need(q.of((int)r) == r / d, "quotient", r, d);
+  }
+  for (long long rows : {1ll, 8ll, 128000ll, 1ll << 30})
+    for (long long n : {1ll, 6ll, 64ll, 65535ll}) need(append_times(148, n, rows, 32) >= 1 && append_times(148, n, rows, 32) <= kAppendTimes, "times", rows, n);
   return 0;
 }
 """
