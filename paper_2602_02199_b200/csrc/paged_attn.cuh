@@ -593,7 +593,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     // the item's parts lie in consecutive CTAs: its start in the first one's second slot, the others in their first
     constexpr int kPart = paged_part_floats<D, NG>();              // per set of heads: accumulators, then maxima and sums
     const int from = shares.owner(unit0 + kPagedItemUnits), to = shares.owner(unit0 + kPagedItemUnits + n_tiles - 1);
-    // parts of a round of the join: half of the ring; `from`'s lies apart from the others
+    // Many parts come by bulk copies, all at once, into the ring, which is free when nothing is left to do (another SM's part is
+    // 0.9 us away); rounds of half the ring in turn. `from`'s part lies apart from the others.
+    const bool bulk = !more && to - from >= kTeam;
     constexpr int kRound = kStages * paged_stage_bytes<D>() / 2 / (kPart * 4);
     auto fetch = [&](int r) {                                      // one thread: round r, if there is one
       const int q0 = r * kRound, n = min(kRound, to - from + 1 - q0);
@@ -618,7 +620,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
       *s_last = last;
       if (last) {
         a.tickets[item] = 0;                                       // ready for the next call
-        if (!more) {
+        if (bulk) {
           fence_proxy_async_global();                              // the parts are read by bulk copies, which
           fence_proxy_async_smem();                                // overwrite tiles that all warps have done with
           fetch(0);
@@ -648,8 +650,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
           o[mt][3] = fmaf(v.w, e[1], o[mt][3] * f[1]);
         }
       };
-      if (!more) {
-        // the ring is free: parts arrive in its halves in turn
+      if (bulk) {
         for (int r = 0; r * kRound <= to - from; ++r) {
           const int n = min(kRound, to - from + 1 - r * kRound);
           const bool landed = mbar_wait(bar_join(r & 1), (uint32_t)(r >> 1) & 1u);
@@ -685,7 +686,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
 // head after head, fetched every sector four times over: 21 us for 131,000 entries of four KV heads); Gs / 4 lanes share an
 // entry and add up. A warp has two such reads, a Gs / 4th of a tile. The rest is a chain of round trips: what a tile is, with its scores; the
 // entries' pages and the normalisers; the old weights, which the attention kernel's producers have asked the L2 cache for.
-constexpr int kPagedWeightsCtas = 5;                       // per SM
+constexpr int kPagedWeightsCtas = 4;                       // per SM
 __global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(const PagedAttnArgs a) {
   const PagedPool& p = a.pool;
   const int lane = threadIdx.x & 31, share = a.Gs / 4, share_shift = 31 - __clz(share);   // lanes of an entry, parts of a tile
@@ -693,19 +694,19 @@ __global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(c
   grid_dependency_wait();
   allow_dependents();
   const int total = *a.score_units;
-  const long long parts = (long long)a.score_tiles << share_shift;
-  auto load = [&](long long part, int2& at, float4 (&x)[2]) {        // behind the units in use lies what an earlier call left
-    part = part < parts ? part : parts - 1;
+  const int parts = a.score_tiles << share_shift;          // of a kilobyte each
+  auto load = [&](int part, int2& at, float4 (&x)[2]) {    // behind the units in use lies what an earlier call left
+    part = min(part, parts - 1);
     at = __ldcg(a.score_at + (part >> share_shift));
-    const float4* src = reinterpret_cast<const float4*>(a.scores) + part * 64 + lane;
+    const float4* src = reinterpret_cast<const float4*>(a.scores) + (long long)part * 64 + lane;
     x[0] = __ldcg(src);
     x[1] = __ldcg(src + 32);
   };
-  long long part = blockIdx.x * 8 + (threadIdx.x >> 5);
+  int part = blockIdx.x * 8 + (threadIdx.x >> 5);
   int2 at_next;
   float4 x_next[2];
   load(part, at_next, x_next);
-  const long long n_parts = (long long)min(total, a.score_tiles) << share_shift;
+  const int n_parts = min(total, a.score_tiles) << share_shift;
   for (; part < n_parts; part += gridDim.x * 8) {
     const int2 at = at_next;
     const float4 x[2] = {x_next[0], x_next[1]};
@@ -713,24 +714,24 @@ __global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(c
     const int b = at.x & 0xFFFF, h = (int)((unsigned)at.x >> 16);
     if (at.y < 0 || b >= p.n_seqs || h >= p.H) continue;   // a unit of an item itself, or the attention gave up
     const float* z = a.lse2 + ((long long)b * p.H + h) * a.G;
-    const int len = p.length(b), first = at.y * kDecTile + ((int)(part & (share - 1)) * 64 + lane) / share;
+    const int len = p.length(b), first = at.y * kDecTile + (((part & (share - 1)) * 64 + lane) >> share_shift);
     int page[2];
     float zz[4], *dst[2], old[2];
     bool ok[2];
 #pragma unroll
-    for (int k = 0; k < 2; ++k) page[k] = p.page(b, min(first + k * 32 / share, (p.max_pages << p.page_shift) - 1));
+    for (int k = 0; k < 2; ++k) page[k] = p.page(b, min(first + (k * 32 >> share_shift), (p.max_pages << p.page_shift) - 1));
 #pragma unroll
     for (int j = 0; j < 4; ++j) zz[j] = z[min(4 * quad + j, a.G - 1)];   // through L1: thousands of warps ask for the same few
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const int i = first + k * 32 / share;
+      const int i = first + (k * 32 >> share_shift);
       ok[k] = i < len && (unsigned)page[k] < (unsigned)p.n_pages && quad == 0;   // bad pages were recorded by the attention
       dst[k] = a.weights + (ok[k] ? (((long long)page[k] * p.H + h) << p.page_shift) + (i & (p.page_size() - 1)) : 0);
       old[k] = *dst[k];
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const float e[4] = {exp2f(x[k].x - zz[0]), exp2f(x[k].y - zz[1]), exp2f(x[k].z - zz[2]), exp2f(x[k].w - zz[3])};
+      const float e[4] = {ex2_approx(x[k].x - zz[0]), ex2_approx(x[k].y - zz[1]), ex2_approx(x[k].z - zz[2]), ex2_approx(x[k].w - zz[3])};
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) if (4 * quad + j < a.G) sum += e[j];

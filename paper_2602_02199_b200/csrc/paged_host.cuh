@@ -63,7 +63,7 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
   // Pages that no two sequences share bound the entries of all sequences together.
   const long long all = (long long)c->n_seqs * seq_tiles, pooled = (long long)c->n_pages * c->page_size / kDecTile + (1 + kPagedItemUnits) * (long long)c->n_seqs;
   const long long tiles = (all < pooled ? all : pooled) * c->n_kv_heads;
-  if (tiles > 0x7fffffffLL) return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: too many entries");
+  if (tiles * (c->n_q_heads / c->n_kv_heads + 3) > 0x3fffffffLL && c->track_weights) return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: too many entries");
   d->score_tiles = c->track_weights ? (int)tiles : 0;
   d->n_moves = c->track_weights ? rows / 2 + 1 : 0;
   for (d->score_heads = 4; d->score_heads < d->group;) d->score_heads *= 2;
