@@ -523,7 +523,8 @@ typedef struct {
 
 laser_kv_status_t laser_kv_paged_query_sizes(const laser_kv_paged_config_t* cfg, size_t* workspace_bytes);
 
-/* Makes the handle's device current, clears the workspace's counters and reads nothing else. CAPACITY for a short workspace. */
+/* Makes the handle's device current, clears the workspace's counters and reads nothing else; not to be captured into a graph.
+ * CAPACITY for a short workspace. */
 laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* k_pages, void* v_pages,
                                       const int64_t kv_strides[3], float* weights, int32_t* pos,
                                       const int32_t* page_table, int32_t* state, void* workspace,
@@ -548,7 +549,8 @@ laser_kv_status_t laser_kv_paged_append(laser_kv_paged_handle_t h, const void* K
 /* Attention of one new token per sequence over the sequence's entries: for query head hq of KV head h = hq / G,
  *   x_i = <Q[b][hq], K_i> * scale,  lse[b][hq] = log sum_i exp(x_i),  out[b][hq][:] = sum_i exp(x_i - lse) V_i.
  * A sequence without entries has out 0 and lse -inf. Products and sums in fp32, rounded once to the output's type; sums over
- * entries are formed in an order that depends on the lengths and the device's SMs alone.
+ * entries are formed in an order that depends on the lengths and the device's SMs alone. An infinity or NaN among a head's held keys, values or
+ * queries can make that head's results NaN, and its entries' weights; it reaches no other head.
  *   Q          : dev, config.dtype, element (b, hq, :) at Q + b*q_strides[0] + hq*q_strides[1]; 16-byte aligned, strides multiples of 8.
  *   softmax_scale : 0 selects 1/sqrt(head_dim).
  *   accumulate : nonzero: every entry's weight grows by sum over the G heads of exp(x_i - lse). ERR_STATE when the cache keeps none.

@@ -27,10 +27,12 @@ def _bits(x):
     ([0], 1001, None, 1, 256, 64, "fp16", False, False, False),
     ([0, 7, 31], 33, [0, 33, 20], 5, 256, 8, "bf16", True, False, True),
     ([100, 0, 40], 515, [515, 0, 77], 4, 64, 128, "bf16", False, True, True),
+    ([5] * 40, 700, [(37 * i) % 90 for i in range(40)], 7, 128, 16, "bf16", False, True, False),   # padded far beyond the tables
+    ([0, 9000], 9001, [9001, 1], 2, 64, 4096, "fp16", True, True, False),
 ])
 def test_append_against_plain_copies(lens, m, counts, H, D, page_size, dtype, token_major, weights, given):
     n = len(lens)
-    most = max(x + m for x in lens)
+    most = max(x + c for x, c in zip(lens, counts or [m] * n))
     cache, gen = build(lens, H=H, G=1, D=D, page_size=page_size, dtype=dtype, token_major=token_major, weights=weights,
                        max_pages=-(-most // page_size), whole_table=True, seen=[x + 10 for x in lens])
     k, v = _new(gen, n, H, m, D, cache.k_pages.dtype, not token_major)

@@ -27,6 +27,8 @@ EDGES = [0, 1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 1000]
     (128, 1, 5, 32, False, [0, 0, 0]),                    # nothing at all
     (128, 3, 1, 16, True, [5000, 0, 1, 64]),
     (64, 70, 1, 16, False, [100, 3000]),                  # five readings, more heads than a warp has lanes
+    (128, 4, 1, 4096, False, [5000, 4096, 4095, 1]),
+    (64, 2, 2, 1024, True, [1025, 2048, 70]),
 ])
 def test_attention_against_64_bits(dtype, D, G, H, page_size, token_major, lens):
     cache, gen = build(lens, H=H, G=G, D=D, page_size=page_size, dtype=dtype, token_major=token_major)
@@ -175,6 +177,34 @@ def test_two_caches_on_two_streams():
     for i, (cache, q, (want, _, _, t_out, _, _), _) in enumerate(pairs):
         for out in outs[i]:
             assert ((out.double() - want).abs() <= t_out).all() and torch.equal(out, outs[i][0])
+
+
+def test_keys_and_values_in_one_allocation():
+    """[n_pages][2][H][page_size][d], one page's keys beside its values, at an offset into a larger buffer."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    both = torch.randn(40 * 2 * 3 * 16 * 128 + 8, generator=gen, device="cuda").half()[8:].view(40, 2, 3, 16, 128)
+    table = torch.randperm(40, generator=gen, device="cuda").to(torch.int32).view(4, 10)
+    state = torch.tensor([[160, 3, 0, 77]] * 2, dtype=torch.int32, device="cuda")
+    cache = Bn.PagedKV(both[:, 0], both[:, 1], table, n_q_heads=15, weights=torch.zeros(40, 3, 16, device="cuda"), state=state)
+    check_attention(cache, queries(cache, gen), accumulate=True)
+    k, v = (torch.randn(4, 3, 1, 128, generator=gen, device="cuda").half() for _ in range(2))
+    cache.lens[0] = 159
+    cache.laser_kv_paged_append(k, v)
+    check_attention(cache, queries(cache, gen), accumulate=True)
+    cache.laser_kv_paged_evict(60)
+    check_attention(cache, queries(cache, gen), out_dtype=torch.float16)
+
+
+def test_queries_that_are_not_numbers_stay_in_their_head():
+    for G, bad in ((4, math.nan), (16, math.inf), (7, -math.inf)):
+        cache, gen = build([300, 70], H=2, G=G, page_size=16)
+        q = queries(cache, gen)
+        good = cache.laser_kv_paged_attention(q).clone()
+        q[0, 1, 5] = bad
+        out = cache.laser_kv_paged_attention(q)
+        keep = torch.ones(2, 2 * G, dtype=torch.bool, device="cuda")
+        keep[0, 1] = False
+        assert torch.equal(out[keep], good[keep]) and torch.isnan(out[0, 1]).all()
 
 
 def test_pages_that_sequences_share():

@@ -30,6 +30,7 @@ def _evict(cache, keep, anchors=0, recent=0):
     ([600, 50], 1, 256, 128, "bf16", False, 599, 1, 1),
     ([40000, 39999], 8, 64, 64, "fp16", False, 20000, 1000, 5000),
     ([300] * 600, 1, 64, 16, "bf16", False, 200, 3, 50),              # more clusters than SMs
+    ([5000, 4097], 2, 64, 4096, "fp16", True, 4096, 10, 100),
 ])
 def test_evict_against_the_definition(lens, H, D, page_size, dtype, token_major, keep, anchors, recent):
     cache, gen = build(lens, H=H, G=1, D=D, page_size=page_size, dtype=dtype, token_major=token_major)
