@@ -115,9 +115,10 @@ __global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_a
 // shared memory.
 //   1. keys: the weight as an ordered integer, the largest for protected entries (the first positions and the last ones),
 //      -inf for NaN, which therefore leaves first.
-//   2. the keep-th largest key, by radix rounds over the eleven highest bits in which undecided keys can differ (as in
-//      take_topk), the histograms summed across the cluster; protected keys, often the most, are counted apart, so that they
-//      do not pile up in one bin. A lone CTA ranks the last few undecided keys against one another instead of further rounds.
+//   2. the keep-th largest key, by radix rounds over 11, 11 and 10 bits, the histograms summed across the cluster; protected
+//      keys, often the most, are counted apart, so that they do not pile up in one bin. (Starting from the smallest and the largest key, as
+//      take_topk does, takes one more barrier and gains nothing where some entries never received any weight.) A lone CTA ranks
+//      the last few undecided keys against one another instead of further rounds.
 //   3. a sweep in index order with two counts (keys above, keys equal to it) gives every entry its rank among the kept ones.
 //      An evicted entry before `keep` is a hole, a kept one behind it a mover; holes are counted from the start, movers from the end,
 //      and the pairs go to a list, as slots of the pool.
@@ -139,15 +140,12 @@ constexpr int kEvictWarps = kEvictThreads / 32;
 constexpr int kEvictFew = 256;                             // undecided keys that a lone CTA ranks directly
 
 struct EvictShared {
-  int hist[kSelBins];                                      // this CTA's; zero between rounds
-  int sums[kSelBins];                                      // its share of the cluster's bins, summed over the CTAs
+  int hist[2][kSelBins];                                   // this CTA's, of alternate rounds; the next round's is zero
+  int sums[kSelBins];                                      // large clusters: its share of the cluster's bins, summed over the CTAs
   int share;                                               // sum of its share
   int chunk[kEvictWarps];
   int found[3];
-  uint32_t lo[kEvictWarps], hi[kEvictWarps];
-  int prot[kEvictWarps];
-  uint32_t range[2];                                       // smallest and largest unprotected key of the CTA
-  int n_prot, n_few;
+  int n_prot, n_few;                                       // protected entries of the CTA; keys in `few`
   uint32_t few[kEvictFew];
   int above[kEvictWarps], equal[kEvictWarps];
   int totals[2];                                           // CTA: keys above, keys equal
@@ -177,8 +175,9 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
   const int C = gridDim.x, rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   auto remote = [&](const void* at, int r) { return ld_cluster_u32(cluster_addr(smem_u32(at), r)); };
-  for (int i = tid; i < kSelBins; i += kEvictThreads) sh.hist[i] = 0;
-  if (tid == 0) sh.n_few = 0;
+  for (int i = tid; i < 2 * kSelBins; i += kEvictThreads) sh.hist[0][i] = 0;
+  if (tid == 0) sh.n_prot = sh.n_few = 0;
+  __syncthreads();
   grid_dependency_wait();
   allow_dependents();
 
@@ -202,7 +201,7 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
 
   // ---- 1. keys ----------------------------------------------------------------------------------
   const int slice = evict_slice(len, C), lo_i = min(len, rank * slice), n = min(len - lo_i, slice);
-  uint32_t lo = 0xFFFFFFFFu, hi = 0u;
+  constexpr int kFirst = 32 - kSelBinBits;                 // the first round's bins: the highest bits
   int prot = 0;
   constexpr int kAtOnce = 4;                               // keys of a thread under way together: nothing is loaded under a condition
   for (int i0 = tid; i0 < n; i0 += kAtOnce * kEvictThreads) {
@@ -228,25 +227,13 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
       const uint32_t key = safe ? kEvictProtected : orderable_f32(bad || x[j] != x[j] ? -INFINITY : x[j] + 0.f);   // + 0: -0 is 0
       keys[i] = key;
       prot += safe;
-      if (!safe) { lo = min(lo, key); hi = max(hi, key); }
+      if (!safe) atomicAdd(&sh.hist[0][key >> kFirst], 1);
     }
   }
-  lo = __reduce_min_sync(0xffffffffu, lo);
-  hi = __reduce_max_sync(0xffffffffu, hi);
   prot = __reduce_add_sync(0xffffffffu, prot);
-  if (lane == 0) { sh.lo[warp] = lo; sh.hi[warp] = hi; sh.prot[warp] = prot; }
-  __syncthreads();
-  lo = __reduce_min_sync(0xffffffffu, sh.lo[lane % kEvictWarps]);
-  hi = __reduce_max_sync(0xffffffffu, sh.hi[lane % kEvictWarps]);
-  prot = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.prot[lane] : 0);
-  if (C > 1) {
-    if (tid == 0) { sh.range[0] = lo; sh.range[1] = hi; sh.n_prot = prot; }
-    cluster_sync();
-    const int r = lane < C ? lane : 0;
-    lo = __reduce_min_sync(0xffffffffu, remote(&sh.range[0], r));
-    hi = __reduce_max_sync(0xffffffffu, remote(&sh.range[1], r));
-    prot = __reduce_add_sync(0xffffffffu, lane < C ? (int)remote(&sh.n_prot, r) : 0);
-  }
+  if (lane == 0 && prot) atomicAdd(&sh.n_prot, prot);
+  if (C > 1) cluster_sync(); else __syncthreads();         // the first histograms and the numbers of protected entries are there
+  prot = __reduce_add_sync(0xffffffffu, lane < C ? (int)remote(&sh.n_prot, lane) : 0);
 
   // ---- 2. the keep-th largest key ----------------------------------------------------------------
   // kept: keys from `from` on, and of those equal to `tie` the first `ties` in index order
@@ -257,20 +244,36 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
     ties = keep;                                           // of the protected ones themselves
   } else {
     int need = keep - prot;                                // of len - prot > need unprotected ones
-    uint32_t base = lo;
-    uint64_t span_hi = hi;                                 // undecided: keys in [base, span_hi]
-    int shift = 32 - __clz(hi - lo) - kSelBinBits;
-    if (shift < 0) shift = 0;
-    const int per = kSelBins / C;                          // bins of a CTA's share
-    for (;;) {
-      for (int i = tid; i < n; i += kEvictThreads) {
-        const uint32_t key = keys[i];
-        if (key != kEvictProtected && key >= base && key <= span_hi) atomicAdd(&sh.hist[(key - base) >> shift], 1);
+    uint32_t base = 0, last = kEvictProtected - 1u;        // undecided: keys in [base, last]
+    int shift = kFirst;                                    // a bin has 2^shift of them
+    const int per = kSelBins / C;                          // large clusters: bins of a CTA's share
+    for (int round = 0;; ++round) {
+      int* const hist = sh.hist[round & 1];
+      if (round > 0) {
+        for (int i = tid; i < n; i += kEvictThreads) {
+          const uint32_t key = keys[i];
+          if (key >= base && key <= last) atomicAdd(&hist[(key - base) >> shift], 1);
+        }
+        if (C > 1) cluster_sync(); else __syncthreads();
       }
-      const int* bins = sh.hist;
-      int share = 0, before = 0;
-      if (C > 1) {
-        cluster_sync();
+      // bins from high to low, a warp takes a run of them: of the whole histogram, which every CTA of a small cluster adds up for
+      // itself, or of the share that holds the need-th from the top
+      constexpr int kMost = kSelBins / kEvictThreads;
+      int c[kMost], bins = kSelBins, share = 0, before = 0;
+      if (C <= 4) {
+#pragma unroll
+        for (int k = 0; k < kMost; ++k) {
+          const int i = kSelBins - 1 - (tid * kMost + k);
+          c[k] = C == 1 ? hist[i] : 0;
+          if (C > 1) {
+            int x[4];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[r] = (int)remote(&hist[i], min(r, C - 1));   // together
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (r < C) c[k] += x[r];
+          }
+        }
+      } else {
         // this CTA's share: bins [rank * per, (rank + 1) * per)
         int mine = 0;
         for (int i = tid; i < per; i += kEvictThreads) {
@@ -278,7 +281,7 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
           for (int r0 = 0; r0 < C; r0 += 4) {              // four reads under way together
             int x[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) x[r] = (int)remote(&sh.hist[rank * per + i], min(r0 + r, C - 1));
+            for (int r = 0; r < 4; ++r) x[r] = (int)remote(&hist[rank * per + i], min(r0 + r, C - 1));
 #pragma unroll
             for (int r = 0; r < 4; ++r) if (r0 + r < C) v += x[r];
           }
@@ -292,31 +295,25 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
           const int s = __reduce_add_sync(0xffffffffu, lane < kEvictWarps ? sh.chunk[lane] : 0);
           if (lane == 0) sh.share = s;
         }
-        cluster_sync();                                    // sums are written, histograms read
-        // the share that holds the need-th from the top
+        cluster_sync();                                    // sums are written
         const int v = lane < C ? (int)remote(&sh.share, C - 1 - lane) : 0;
         const int incl = warp_inclusive(v, lane);
-        const int who = __ffs(__ballot_sync(0xffffffffu, lane < C && incl >= need)) - 1;
+        const int who = (__ffs(__ballot_sync(0xffffffffu, lane < C && incl >= need)) - 1) & 31;
         share = C - 1 - who;
         before = __shfl_sync(0xffffffffu, incl - v, who);
-        bins = nullptr;
-      } else {
-        __syncthreads();
-      }
-      // bins of the share from high to low; a warp takes a run of them
-      constexpr int kMost = kSelBins / kEvictThreads;
-      const int mine_n = (per + kEvictThreads - 1) / kEvictThreads;
-      int c[kMost], sum = 0;
+        bins = per;
 #pragma unroll
-      for (int k = 0; k < kMost; ++k) {
-        const int i = per - 1 - (tid * mine_n + k);
-        c[k] = k < mine_n && i >= 0 ? (bins ? bins[i] : (int)remote(&sh.sums[i], share)) : 0;
-        sum += c[k];
+        for (int k = 0; k < kMost; ++k) c[k] = 0;
+        if (tid < per) c[0] = (int)remote(&sh.sums[per - 1 - tid], share);   // per <= kEvictThreads
       }
+      int sum = 0;
+#pragma unroll
+      for (int k = 0; k < kMost; ++k) sum += c[k];
       const int wsum = __reduce_add_sync(0xffffffffu, sum);
-      __syncthreads();                                     // sh.chunk is read (share sums), the bins too
+      // the other histogram: all of the cluster have read it, in the round before this one's barrier
+      for (int i = tid; i < kSelBins; i += kEvictThreads) sh.hist[(round + 1) & 1][i] = 0;
+      __syncthreads();                                     // sh.chunk is read
       if (lane == 0) sh.chunk[warp] = wsum;
-      for (int i = tid; i < kSelBins; i += kEvictThreads) sh.hist[i] = 0;
       __syncthreads();
       {
         const int x = lane < kEvictWarps ? sh.chunk[lane] : 0;
@@ -326,7 +323,7 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
 #pragma unroll
         for (int k = 0; k < kMost; ++k) {
           if (run < need && need <= run + c[k]) {
-            sh.found[0] = share * per + per - 1 - (tid * mine_n + k);
+            sh.found[0] = C <= 4 ? kSelBins - 1 - (tid * kMost + k) : share * per + bins - 1 - tid;
             sh.found[1] = need - run;
             sh.found[2] = c[k];
           }
@@ -348,12 +345,12 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
         ties = need;
         break;
       }
-      span_hi = (uint64_t)base + (1ull << shift) - 1;
+      last = base + (1u << shift) - 1u;                    // below kEvictProtected
       if (C == 1 && held_in <= kEvictFew) {
         for (int i0 = warp * 32; i0 < n; i0 += kEvictThreads) {
           const int i = i0 + lane;
           const uint32_t key = i < n ? keys[i] : kEvictProtected;
-          const bool in = key != kEvictProtected && key >= base && key <= span_hi;
+          const bool in = key >= base && key <= last;
           const uint32_t mask = __ballot_sync(0xffffffffu, in);
           int at = 0;
           if (lane == 0 && mask) at = atomicAdd(&sh.n_few, __popc(mask));
@@ -380,7 +377,7 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
         from = tie + 1;
         break;
       }
-      shift = shift > kSelBinBits ? shift - kSelBinBits : 0;
+      shift -= shift > kSelBinBits ? kSelBinBits : shift;  // 21, 10, 0
     }
   }
 
