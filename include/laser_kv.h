@@ -523,7 +523,7 @@ typedef struct {
 
 laser_kv_status_t laser_kv_paged_query_sizes(const laser_kv_paged_config_t* cfg, size_t* workspace_bytes);
 
-/* Makes the handle's device current, clears the workspace's counters and reads nothing else; not to be captured into a graph.
+/* Makes the handle's device current and clears the workspace's counters, for which it waits for the device; not to be captured into a graph.
  * CAPACITY for a short workspace. */
 laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* k_pages, void* v_pages,
                                       const int64_t kv_strides[3], float* weights, int32_t* pos,

@@ -208,7 +208,8 @@ laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* 
     if (counts[i] == 1) strides[i] = cfg->head_dim;              // never stepped over
     if (strides[i] < cfg->head_dim || (strides[i] % 8))
       return fail(nullptr, LASER_KV_ERR_ALIGNMENT, "paged_init: strides must be multiples of 8 elements, a row at least");
-    if (strides[i] >= (1ll << 38)) return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged_init: stride of 2^38 elements or more");
+    if (strides[i] >= (1ll << 38) || (double)strides[i] * (double)counts[i] > 1e15)
+      return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged_init: stride of 2^38 elements or more, or a pool of 1e15");
   }
   if (!paged_disjoint(cfg->head_dim, strides, counts)) return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "paged_init: the strides make rows overlap");
   if (workspace_bytes < d.total) return fail(nullptr, LASER_KV_ERR_CAPACITY, "paged_init: workspace needs %zu bytes, got %zu", d.total, workspace_bytes);
@@ -259,8 +260,10 @@ laser_kv_status_t laser_kv_paged_init(const laser_kv_paged_config_t* cfg, void* 
   laser_kv_status_t bad = LASER_KV_OK;
   if (!paged_map(enc, &h->map_k, *cfg, k_pages, strides) || !paged_map(enc, &h->map_v, *cfg, v_pages, strides))
     bad = fail(nullptr, LASER_KV_ERR_CUDA, "paged_init: cuTensorMapEncodeTiled failed");
-  else if ((e = cudaMemset(ws, 0, d.zeroed)) != cudaSuccess)
-    bad = fail(nullptr, LASER_KV_ERR_CUDA, "paged_init: cudaMemset: %s", cudaGetErrorString(e));
+  else if ((e = cudaDeviceSynchronize()) != cudaSuccess ||     // whatever used this memory before is done with it, on any stream
+           (e = cudaMemset(ws, 0, d.zeroed)) != cudaSuccess ||
+           (e = cudaDeviceSynchronize()) != cudaSuccess)         // the first call may come on a stream that does not wait for this one
+    bad = fail(nullptr, LASER_KV_ERR_CUDA, "paged_init: clearing the counters: %s", cudaGetErrorString(e));
   if (bad != LASER_KV_OK) {
     delete h;
     return bad;

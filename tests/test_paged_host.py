@@ -75,6 +75,8 @@ def test_init_refuses_what_it_can_see():
         assert init(st=st) == Bn.ERR_ALIGNMENT
     for st in ((8 * 16 * 128, 8 * 128, 128), (7 * 16 * 128, 16 * 128, 128), (128, 128, 128), (8 * 16 * 128 - 8, 128, 8 * 128)):
         assert init(st=st) == Bn.ERR_INVALID_ARG and "overlap" in _message()
+    assert init(st=(1 << 38, 16 * 128, 128)) == Bn.ERR_UNSUPPORTED
+    assert init(cfg=_cfg(n_pages=1 << 16), bytes=1 << 50, st=(1 << 37, 16 * 128, 128)) == Bn.ERR_UNSUPPORTED
     # rows that lie beside one another in any order of the strides; a dimension of one entry has no stride
     for st, kw in (((8 * 16 * 128, 128, 8 * 128), {}), ((128, 64 * 128, 8 * 64 * 128), {}), ((16 * 128, 8, 128), dict(n_kv_heads=1, n_q_heads=4)),
                    ((3 * 8 * 16 * 128, 16 * 136, 136), {})):
