@@ -127,7 +127,8 @@ struct PagedWalk {
   int len, n_tiles;                                        // of the sequence
   int before;                                              // units per item of the sequences before this one
   int unit0;                                               // the item's first unit
-  __device__ __forceinline__ int units() const { return n_tiles + kPagedItemUnits; }
+  bool whole;                                              // all items count alike
+  __device__ __forceinline__ int units() const { return whole ? kPagedWholeUnits : n_tiles + kPagedItemUnits; }
   // The item's tiles in the units [begin, stop) are [first, last); none where first >= last.
   __device__ __forceinline__ int first(int begin) const { return max(0, begin - unit0 - kPagedItemUnits); }
   __device__ __forceinline__ int last(int stop) const { return min(n_tiles, stop - unit0 - kPagedItemUnits); }
@@ -147,7 +148,9 @@ struct PagedWalk {
   }
 };
 
-__device__ __forceinline__ int paged_units(int len) { return len > 0 ? (len + kDecTile - 1) / kDecTile + kPagedItemUnits : 0; }
+__device__ __forceinline__ int paged_units(int len, bool whole) {
+  return len <= 0 ? 0 : whole ? kPagedWholeUnits : (len + kDecTile - 1) / kDecTile + kPagedItemUnits;
+}
 
 __device__ __forceinline__ int warp_inclusive(int x, int lane) {
 #pragma unroll
@@ -161,22 +164,29 @@ __device__ __forceinline__ int warp_inclusive(int x, int lane) {
 // or, of more than 32, as many blocks of 32 as it takes.
 struct PagedSum {
   int per, incl, mine, total, len;                         // len: the lane's only sequence's, where per is 1
+  bool whole;                                              // no sequence has more than kPagedWhole tiles
   __device__ __forceinline__ PagedSum(const PagedPool& p, int lane) {
+    int longest = 0;
+    len = 0;
     if (p.n_seqs <= 32) {
       per = 1;
-      len = lane < p.n_seqs ? p.length(lane) : 0;
-      mine = paged_units(len);
+      len = longest = lane < p.n_seqs ? p.length(lane) : 0;
+      whole = __reduce_max_sync(0xffffffffu, longest) <= kPagedWhole * kDecTile;
+      mine = paged_units(len, whole);
     } else {
       const int blocks = (p.n_seqs + 1023) >> 10;          // of a lane
       per = 32 * blocks;
-      mine = len = 0;
+      int all = 0, alike = 0;
       const int n = (p.n_seqs + 31) >> 5;
 #pragma unroll 4
       for (int k = 0; k < n; ++k) {
-        const int i = min(32 * k + lane, p.n_seqs - 1), u = paged_units(p.length(i));
-        const int s = __reduce_add_sync(0xffffffffu, 32 * k + lane < p.n_seqs ? u : 0);
-        if (k / blocks == lane) mine += s;
+        const int x = p.length(min(32 * k + lane, p.n_seqs - 1)), here = 32 * k + lane < p.n_seqs ? x : 0;
+        longest = max(longest, here);
+        const int s = __reduce_add_sync(0xffffffffu, paged_units(here, false)), w = kPagedWholeUnits * __popc(__ballot_sync(0xffffffffu, here > 0));
+        if (k / blocks == lane) { all += s; alike += w; }
       }
+      whole = __reduce_max_sync(0xffffffffu, longest) <= kPagedWhole * kDecTile;
+      mine = whole ? alike : all;
     }
     incl = warp_inclusive(mine, lane);
     total = __shfl_sync(0xffffffffu, incl, 31);
@@ -190,10 +200,11 @@ __device__ __forceinline__ PagedWalk paged_seek(const PagedPool& p, int lane, co
   w.before = __shfl_sync(0xffffffffu, sum.incl - sum.mine, who);
   w.b = who * sum.per;
   w.len = __shfl_sync(0xffffffffu, sum.len, who);
+  w.whole = sum.whole;
   if (sum.per > 1) {
     for (;;) {
       const int i = w.b + lane;
-      const int len = i < p.n_seqs ? p.length(i) : 0, u = paged_units(len);
+      const int len = i < p.n_seqs ? p.length(i) : 0, u = paged_units(len, sum.whole);
       const int incl = w.before + warp_inclusive(u, lane);
       const uint32_t found = __ballot_sync(0xffffffffu, incl > q);
       if (found || w.b + 32 >= p.n_seqs) {                 // `at` is in the list: found
@@ -276,7 +287,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   allow_dependents();
 
   const PagedSum sum(p, lane);
-  const PagedShares shares(sum.total * heads, (int)gridDim.x);
+  const PagedShares shares(sum.total * heads, (int)gridDim.x, sum.whole);
   const int cta = blockIdx.x;
   const int begin = cta < shares.n ? shares.begin(cta) : 0, stop = cta < shares.n ? shares.begin(cta + 1) : 0;
   bool more = begin < stop;
@@ -472,7 +483,9 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
     const int h = w.head / a.head_blocks;
     clear();
     const int score_unit = w.before * p.H + h * w.units();           // of the item
-    if (a.scores && tid < (t0 == 0 ? kPagedItemUnits : 0) && score_unit + tid < a.score_tiles) a.score_at[score_unit + tid] = make_int2(0, -1);
+    if (a.scores && t0 == 0 && tid < kPagedWholeUnits && (tid < kPagedItemUnits || (w.whole && tid >= kPagedItemUnits + w.n_tiles)) &&
+        score_unit + tid < a.score_tiles)
+      a.score_at[score_unit + tid] = make_int2(0, -1);               // units that are no tiles
     for (int t = t0; t < t1; ++t) {
       if (!gone && !__all_sync(0xffffffffu, mbar_wait(bar_full(st), (uint32_t)round & 1u))) {
         if (lane == 0) record_status(p.status, kStatusTimeout);

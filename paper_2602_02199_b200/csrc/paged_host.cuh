@@ -54,14 +54,14 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
   d->group = c->n_q_heads / c->n_kv_heads;
   d->n_wide = d->group <= 8 ? 1 : 2;
   d->head_blocks = (d->group + 8 * d->n_wide - 1) / (8 * d->n_wide);
-  const long long seq_tiles = (d->cap + kDecTile - 1) / kDecTile + kPagedItemUnits;
+  const long long seq_tiles = (d->cap + kDecTile - 1) / kDecTile + kPagedWholeUnits;   // units at most
   if (c->n_seqs > 65535 || c->n_kv_heads > 65535 || d->cap > (1ll << 30) || rows > 0x7fffffffLL ||
       (double)c->n_seqs * c->n_kv_heads * d->head_blocks * (double)seq_tiles > 2147483647.0 ||
       (double)c->n_seqs * c->n_q_heads > 2147483647.0)
     return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: more than 65535 sequences or KV heads, 2^30 entries per sequence or 2^31 rows or tiles");
   for (d->page_shift = 3; (1 << d->page_shift) < c->page_size;) ++d->page_shift;
   // Pages that no two sequences share bound the entries of all sequences together.
-  const long long all = (long long)c->n_seqs * seq_tiles, pooled = (long long)c->n_pages * c->page_size / kDecTile + (1 + kPagedItemUnits) * (long long)c->n_seqs;
+  const long long all = (long long)c->n_seqs * seq_tiles, pooled = (long long)c->n_pages * c->page_size / kDecTile + kPagedWholeUnits * (long long)c->n_seqs;
   const long long tiles = (all < pooled ? all : pooled) * c->n_kv_heads;
   if (tiles * (c->n_q_heads / c->n_kv_heads + 3) > 0x3fffffffLL && c->track_weights) return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: too many entries");
   d->score_tiles = c->track_weights ? (int)tiles : 0;

@@ -26,6 +26,8 @@ EDGES = [0, 1, 2, 7, 8, 9, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200, 1000]
     (256, 9, 1, 8, False, [129, 5, 0]),
     (128, 1, 5, 32, False, [0, 0, 0]),                    # nothing at all
     (128, 3, 1, 16, True, [5000, 0, 1, 64]),
+    (128, 4, 3, 16, False, [256, 255, 0, 193, 1]),        # no item is split: up to four tiles
+    (64, 9, 2, 8, True, [257, 100, 256]),
     (64, 70, 1, 16, False, [100, 3000]),                  # five readings, more heads than a warp has lanes
     (128, 4, 1, 4096, False, [5000, 4096, 4095, 1]),
     (64, 2, 2, 1024, True, [1025, 2048, 70]),
@@ -41,9 +43,10 @@ def test_attention_against_64_bits(dtype, D, G, H, page_size, token_major, lens)
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("n", [31, 32, 33, 70, 1023, 1024, 1025, 2500])
 def test_many_sequences(dtype, n):
-    lens = [(i * 37) % 190 if i % 5 else 0 for i in range(n)]
-    cache, gen = build(lens, H=2, G=2, D=64, page_size=16, dtype=dtype)
-    check_attention(cache, queries(cache, gen), accumulate=True)
+    for most in (190, 257, 500):
+        lens = [(i * 37) % most if i % 5 else 0 for i in range(n)]
+        cache, gen = build(lens, H=2, G=2, D=64, page_size=16, dtype=dtype)
+        check_attention(cache, queries(cache, gen), accumulate=True)
 
 
 @pytest.mark.parametrize("D,H,lens", [(64, 1, [200001]), (128, 1, [70000, 3, 33333]), (256, 2, [20011])])
@@ -245,9 +248,9 @@ def test_bad_pages_and_lengths_are_reported_and_go_no_further():
 
 def test_weights_of_shared_pages_are_refused_where_they_do_not_fit():
     """Sequences of a cache with weights that share pages can hold more entries than the pool: reported, nothing is written past the room."""
-    cache, gen = build([256] + [0] * 39, H=1, G=2, page_size=64, spare=0)
+    cache, gen = build([1024] + [0] * 39, H=1, G=2, page_size=64, spare=0)
     cache.page_table[:] = cache.page_table[0]
-    cache.lens[:] = 256
+    cache.lens[:] = 1024
     out = cache.laser_kv_paged_attention(queries(cache, gen), accumulate=True)
     assert torch.isfinite(out).all()
     with pytest.raises(Bn.LaserKVError) as e:

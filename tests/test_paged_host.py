@@ -50,7 +50,7 @@ def test_workspace_sizes(group, track, d):
     least = ctas * 2 * wide * 8 * (d + 2) * 4
     if track:
         heads = max(4, 1 << (group - 1).bit_length())
-        units = (64 * 16 // 64 + 3 * 4) * 8
+        units = (64 * 16 // 64 + 6 * 4) * 8
         least += units * (64 * heads * 4 + 8) + 64 * 16 * 8 // 2 * 8
     assert least <= size <= least + 20000
 
@@ -122,7 +122,7 @@ int main() {
   const int totals[] = {1, 2, 3, 7, 147, 148, 149, 295, 296, 297, 1000, 4097, 123457, 2147483647};
   for (int total : totals)
     for (int grid : {1, 2, 3, 148, 296, 444, 480}) {
-      const PagedShares s(total, grid);
+      const PagedShares s(total, grid, false);
       const int n = s.n;
       need(n >= 1 && n <= grid && n <= total, "shares", total, grid);
       need(s.begin(0) == 0 && s.begin(n) == total, "ends", total, n);
@@ -132,7 +132,13 @@ int main() {
         need(s.owner(lo) == c && s.owner(hi - 1) == c && s.owner(lo + (hi - lo) / 2) == c, "owner", total, c);
       }
     }
-  need(PagedShares(0, 296).n == 0, "no tiles", 0, 0);
+  need(PagedShares(0, 296, false).n == 0 && PagedShares(0, 296, true).n == 0, "no tiles", 0, 0);
+  for (int items : {1, 2, 7, 295, 296, 297, 5000, 268435455})        // none is split
+    for (int grid : {1, 3, 148, 296, 480}) {
+      const PagedShares s(items * kPagedWholeUnits, grid, true);
+      need(s.n >= 1 && s.n <= grid && s.n <= items && s.begin(0) == 0 && s.begin(s.n) == items * kPagedWholeUnits, "whole", items, grid);
+      for (int c = 0; c < s.n; ++c) need(s.begin(c) % kPagedWholeUnits == 0 && s.begin(c + 1) > s.begin(c), "item", items, c);
+    }
   for (long long heads : {1ll, 2ll, 8ll, 30ll, 64ll, 100ll, 512ll, 100000ll})
     for (long long cap : {8ll, 64ll, 1024ll, 1025ll, 2056ll, 40960ll, 49152ll, 49153ll, 400000ll, 786432ll, 786433ll})
       for (int most : {8, 16}) {
