@@ -625,7 +625,9 @@ class PagedKV:
                                             self.workspace.numel(), C.byref(h)))
         self.handle = h
         self._h = h.value                # what the native call path takes; 0 once closed
-        self._device, self._f32, self._i32 = dev, torch.float32, torch.int32
+        self._device, self._index, self._f32, self._i32 = dev, dev.index, torch.float32, torch.int32
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)       # as _current_stream_getter, for the cache's device
+        self._current = _stream_ptr if raw is None else lambda stream, index=dev.index: raw(index) if stream is None else _stream_ptr(stream)
         self._types = (torch.float16,) if k_pages.dtype == torch.float16 else (torch.bfloat16, torch.int16)
         self._q_shape, self._lse_shape = (n_seqs, n_q_heads, d), (n_seqs, n_q_heads)
         self._n_seqs, self._heads, self._d = n_seqs, heads, d
@@ -650,59 +652,59 @@ class PagedKV:
     def laser_kv_paged_append(self, K_new, V_new, counts=None, weights=None, pos=None, stream=None):
         """K_new, V_new: [n_seqs][H_kv][n_new][d] (any strides with a contiguous last dim); counts int32 [n_seqs]; weights fp32 and pos
         int32 [n_seqs][H_kv][n_new] with contiguous last dims."""
-        n_seqs, heads, d, dev, i32 = self._n_seqs, self._heads, self._d, self._device, self._i32
+        n_seqs, heads, d, dev, i32 = self._n_seqs, self._heads, self._d, self._index, self._i32
         kshape, ks, vs = K_new.shape, K_new.stride(), V_new.stride()
         n_new = kshape[2] if len(kshape) == 4 else -1
-        if kshape != (n_seqs, heads, n_new, d) or ks[3] != 1 or K_new.dtype not in self._types or K_new.device != dev:
+        if kshape != (n_seqs, heads, n_new, d) or ks[3] != 1 or K_new.dtype not in self._types or K_new.get_device() != dev:
             self._refuse(K_new, self._types, (n_seqs, heads, n_new, d), "paged_append: K_new")
-        if V_new.shape != kshape or vs[3] != 1 or V_new.dtype not in self._types or V_new.device != dev:
+        if V_new.shape != kshape or vs[3] != 1 or V_new.dtype not in self._types or V_new.get_device() != dev:
             self._refuse(V_new, self._types, kshape, "paged_append: V_new")
         c = w = at = 0
         ws = ps = (0, 0)
         if counts is not None:
-            if counts.shape != (n_seqs,) or counts.dtype != i32 or counts.device != dev or not counts.is_contiguous():
+            if counts.shape != (n_seqs,) or counts.dtype != i32 or counts.get_device() != dev or not counts.is_contiguous():
                 self._refuse(counts, (i32,), (n_seqs,), "paged_append: counts")
             c = counts.data_ptr()
         if weights is not None:
             ws = weights.stride()
-            if weights.shape != (n_seqs, heads, n_new) or weights.dtype != self._f32 or weights.device != dev or (n_new > 1 and ws[2] != 1):
+            if weights.shape != (n_seqs, heads, n_new) or weights.dtype != self._f32 or weights.get_device() != dev or (n_new > 1 and ws[2] != 1):
                 self._refuse(weights, (self._f32,), (n_seqs, heads, n_new), "paged_append: weights")
             w = weights.data_ptr()
         if pos is not None:
             ps = pos.stride()
-            if pos.shape != (n_seqs, heads, n_new) or pos.dtype != i32 or pos.device != dev or (n_new > 1 and ps[2] != 1):
+            if pos.shape != (n_seqs, heads, n_new) or pos.dtype != i32 or pos.get_device() != dev or (n_new > 1 and ps[2] != 1):
                 self._refuse(pos, (i32,), (n_seqs, heads, n_new), "paged_append: pos")
             at = pos.data_ptr()
-        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, c, w, ws, at, ps, _stream_ptr(stream))
+        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, c, w, ws, at, ps, self._current(stream))
         if s:
             _check(s)
 
     def laser_kv_paged_attention(self, Q, softmax_scale=0.0, accumulate=False, out=None, lse=None, stream=None):
         """Q: [n_seqs][H_q][d] of the cache's type (contiguous last dim) -> [n_seqs][H_q][d], fp32 or, where `out` says so, the cache's
         type. `lse`: fp32 [n_seqs][H_q], receives the logarithm of the sum of exponentials."""
-        shape, dev, qs, f32 = self._q_shape, self._device, Q.stride(), self._f32
-        if Q.shape != shape or qs[2] != 1 or Q.dtype not in self._types or Q.device != dev:
+        shape, dev, qs, f32 = self._q_shape, self._index, Q.stride(), self._f32
+        if Q.shape != shape or qs[2] != 1 or Q.dtype not in self._types or Q.get_device() != dev:
             self._refuse(Q, self._types, shape, "paged_attention: Q")
         is32 = 1
         if out is None:
-            out = self._empty(shape, dtype=f32, device=dev)
+            out = self._empty(shape, dtype=f32, device=self._device)
         else:
             is32 = out.dtype == f32
-            if out.shape != shape or not out.is_contiguous() or not (is32 or out.dtype in self._types) or out.device != dev:
+            if out.shape != shape or not out.is_contiguous() or not (is32 or out.dtype in self._types) or out.get_device() != dev:
                 self._refuse(out, (f32,) + self._types, shape, "paged_attention: contiguous out")
         z = 0
         if lse is not None:
-            if lse.shape != self._lse_shape or not lse.is_contiguous() or lse.dtype != f32 or lse.device != dev:
+            if lse.shape != self._lse_shape or not lse.is_contiguous() or lse.dtype != f32 or lse.get_device() != dev:
                 self._refuse(lse, (f32,), self._lse_shape, "paged_attention: contiguous lse")
             z = lse.data_ptr()
         s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(), is32, z,
-                                    _stream_ptr(stream))
+                                    self._current(stream))
         if s:
             _check(s)
         return out
 
     def laser_kv_paged_evict(self, keep, anchors=0, recent=0, stream=None):
-        s = _pycall.paged_evict(self._h, keep, anchors, recent, _stream_ptr(stream))
+        s = _pycall.paged_evict(self._h, keep, anchors, recent, self._current(stream))
         if s:
             _check(s)
 
