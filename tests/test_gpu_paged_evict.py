@@ -31,6 +31,9 @@ def _evict(cache, keep, anchors=0, recent=0):
     ([40000, 39999], 8, 64, 64, "fp16", False, 20000, 1000, 5000),
     ([300] * 600, 1, 64, 16, "bf16", False, 200, 3, 50),              # more clusters than SMs
     ([5000, 4097], 2, 64, 4096, "fp16", True, 4096, 10, 100),
+    ([1087, 1088, 3, 1024, 1025, 0], 5, 256, 32, "bf16", True, 1024, 16, 64),
+    ([1089], 5, 256, 32, "bf16", True, 1024, 16, 64),
+    ([500, 64, 70, 1000], 1, 64, 8, "fp16", False, 64, 3, 5),
 ])
 def test_evict_against_the_definition(lens, H, D, page_size, dtype, token_major, keep, anchors, recent):
     cache, gen = build(lens, H=H, G=1, D=D, page_size=page_size, dtype=dtype, token_major=token_major)
