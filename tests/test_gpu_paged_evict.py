@@ -58,7 +58,7 @@ def test_ties_and_special_weights(values):
         _evict(cache, 0, 0, 0)
 
 
-@pytest.mark.parametrize("lens,H", [([60000], 1), ([60000, 30000], 8), ([400000], 2)])
+@pytest.mark.parametrize("lens,H", [([60000], 1), ([60000, 30000], 8), ([400000], 2), ([786432], 1)])   # the last is as long as a table may be
 def test_heavy_tailed_weights(lens, H):
     """Weights over many octaves, some never attended to; clusters of up to sixteen CTAs."""
     cache, gen = build(lens, H=H, G=1, D=64, page_size=64, stale=None)
