@@ -170,3 +170,33 @@ def test_calls_take_no_device_memory():
     cache.laser_kv_paged_attention(q, accumulate=True, out=out)
     cache.laser_kv_paged_evict(250)
     assert Bn.laser_kv_launch_count() - before == 1 + 1 + 2 + 2
+
+
+def test_a_pool_of_more_than_2_to_the_31_elements():
+    """Pages at the end of a pool whose offsets need more than 32 bits, in bytes and in elements."""
+    n_pages, H, page_size, D = 34000, 8, 64, 128                      # 2.2e9 elements, 4.5 GB a side
+    pool = [torch.zeros(n_pages, H, page_size, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    weights = torch.zeros(n_pages, H, page_size, device="cuda")
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    table = torch.tensor([[n_pages - 1, 3, n_pages - 2, n_pages - 4], [n_pages - 3, n_pages - 5, 0, 7]], dtype=torch.int32, device="cuda")
+    cache = Bn.PagedKV(*pool, table, n_q_heads=4 * H, weights=weights)
+    k, v = (torch.randn(2, H, 250, D, generator=gen, device="cuda").bfloat16() for _ in range(2))
+    w = torch.rand(2, H, 250, generator=gen, device="cuda")
+    cache.laser_kv_paged_append(k, v, weights=w)
+    for b in range(2):
+        page, off = rows(cache, b, 250)
+        assert torch.equal(cache.k_pages[page, :, off].transpose(0, 1), k[b]) and torch.equal(cache.v_pages[page, :, off].transpose(0, 1), v[b])
+        assert torch.equal(cache.weights[page, :, off].T, w[b])
+    check_attention(cache, queries(cache, gen), accumulate=True)
+    before = [x[table.long()].clone() for x in (cache.k_pages, cache.v_pages, cache.weights, cache.pos)]     # [2][4][H][page_size]...
+    cache.laser_kv_paged_evict(100, anchors=4, recent=20)
+    cache.laser_kv_paged_poll_status()
+    s = dict(table=np.arange(8).reshape(2, 4), state=np.array([[250, 250], [250, 250]], dtype=np.int32))
+    for name, x in zip(("k", "v", "w", "pos"), before):
+        x = x.flatten(0, 1)
+        s[name] = (x.view(torch.int16) if x.dtype == torch.bfloat16 else x).cpu().numpy().copy()
+    want = evict_plain(s, page_size, 100, 4, 20)
+    for name, x in zip(("k", "v", "w", "pos"), (cache.k_pages, cache.v_pages, cache.weights, cache.pos)):
+        x = x[table.long()].flatten(0, 1)
+        assert np.array_equal((x.view(torch.int16) if x.dtype == torch.bfloat16 else x).cpu().numpy(), want[name]), name
+    check_attention(cache, queries(cache, gen))
