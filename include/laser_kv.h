@@ -498,7 +498,10 @@ laser_kv_status_t laser_kv_decode_attention(laser_kv_handle_t h, int32_t layer, 
  * What unused slots hold is never interpreted (it may be NaN), and slots that no call is told to write keep it.
  * Lengths, counts and page numbers lie on the device, so the host does not see them: one out of range is not followed (nothing is
  * read or written outside the pool), recorded in the handle's status word, and the results of that sequence are
- * unspecified. laser_kv_paged_poll_status reports it.
+ * unspecified; the others' are what they would be without it. A length out of range counts as none, and is not changed.
+ * Lengths that the tables hold, but the pool does not (more entries in all than it has slots: sequences share pages, or miss some), are
+ * recorded as CAPACITY: then weights of some sequences may not grow in a call that accumulates, and an eviction may leave
+ * sequences as they are. laser_kv_paged_poll_status reports the first of what was recorded.
  * Calls of a handle are asynchronous on `stream`, must be issued to one stream or be ordered by the caller, and may be captured
  * into a graph, which then follows the lengths, table and contents of the replay. They are ordered against other work on the
  * stream as described at laser_kv_select_block. Errors of these calls: laser_kv_last_error(NULL). */

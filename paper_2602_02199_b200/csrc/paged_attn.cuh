@@ -48,9 +48,11 @@ struct PagedPool {                                         // what all kernels o
   int n_seqs, H, n_pages, max_pages, page_shift;
   int* status;
   __device__ __forceinline__ int page_size() const { return 1 << page_shift; }
-  // Entries of a sequence: a length that the table cannot hold is cut.
+  // Entries of a sequence. A length that the table cannot hold counts as none: it takes no part of what sequences share, the list
+  // of tiles, the room for scores and the list of moves.
   __device__ __forceinline__ int length(int b) const {
-    return min(max(lens[b], 0), max_pages << page_shift);
+    const int held = lens[b];
+    return (unsigned)held <= (unsigned)(max_pages << page_shift) ? held : 0;
   }
   __device__ __forceinline__ int page(int b, int i) const { return table[(long long)b * max_pages + (i >> page_shift)]; }
 };

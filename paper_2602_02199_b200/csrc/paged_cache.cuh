@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_a
 //   3. a sweep in index order with two counts (keys above, keys equal to it) gives every entry its rank among the kept ones.
 //      An evicted entry before `keep` is a hole, a kept one behind it a mover; holes are counted from the start, movers from the end,
 //      and the pairs go to a list, as slots of the pool.
-// paged_move_kernel moves rows by the lists, with all SMs, and sets the lengths. All sources lie behind `keep`, all destinations
+// paged_move_kernel moves rows by the lists, with all SMs, and sets the lengths; a sequence whose pairs found no room stays as it is. All sources lie behind `keep`, all destinations
 // before it: no move waits for another, and only rows that have to move are touched. (Closing the gaps in order would move
 // nearly every row.) The first kernel reads 8 bytes per entry and is bound by barriers and round trips, the second by HBM.
 // ------------------------------------------------------------------------------------------------
@@ -132,7 +132,7 @@ struct PagedEvictArgs {
   int keep, anchors, recent;
   int2* moves;                                             // lists of (hole, mover): per sequence, per KV head
   long long n_moves;                                       // pairs that `moves` holds
-  int2* lists;                                             // [n_seqs][H] where each list starts and how long it is
+  int2* lists;                                             // [n_seqs][H] where each list starts (-1: no room for the sequence's) and how long it is
 };
 
 constexpr int kEvictThreads = 1024;
@@ -190,8 +190,8 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) pairs += __shfl_xor_sync(0xffffffffu, pairs, off);
     const long long most = max(0, min(keep, len - keep)), at = pairs * p.H + (long long)h * most;
-    // the list is as large as a pool whose pages are not shared can need
-    if (lane == 0) sh.offset = at + most <= a.n_moves ? (int)at : -1;
+    // the list is as large as a pool whose pages are not shared can need; a sequence goes by all of its heads, in each of them
+    if (lane == 0) sh.offset = (pairs + most) * p.H <= a.n_moves ? (int)at : -1;
   }
   if (len != held && tid == 0) record_status(p.status, kPagedBadPage);
   if (len <= keep) {                                       // the same in all of the cluster
@@ -451,8 +451,8 @@ __global__ void __launch_bounds__(kMoveThreads, 4) paged_move_kernel(const Paged
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 31, l = lane % kLanes;
   grid_dependency_wait();
   allow_dependents();
-  if (blockIdx.x == 0 && h == 0 && tid == 0 && p.lens[b] > a.keep) p.lens[b] = a.keep;   // nothing else here goes by lengths
   const int2 of = a.lists[b * p.H + h];
+  if (blockIdx.x == 0 && h == 0 && tid == 0 && of.x >= 0 && p.length(b) > a.keep) p.lens[b] = a.keep;   // nothing else here goes by lengths
   const int2* const list = a.moves + of.x;
   uint16_t* const side = l < kHalf ? a.rows.K : a.rows.V;
   int* const word = l < kHalf ? reinterpret_cast<int*>(a.rows.weights) : a.rows.pos;     // moved by lanes 0 and kHalf
