@@ -26,7 +26,7 @@ EXPORTS = [
     "laser_kv_set_layer_budget", "laser_kv_set_wait_budget", "laser_kv_window_scores_static_status",
     "laser_kv_lookback_close", "laser_kv_select_tail", "laser_kv_get_counters",
     "laser_kv_paged_query_sizes", "laser_kv_paged_init", "laser_kv_paged_append", "laser_kv_paged_attention",
-    "laser_kv_paged_evict", "laser_kv_paged_poll_status", "laser_kv_paged_destroy",
+    "laser_kv_paged_evict", "laser_kv_paged_poll_status", "laser_kv_paged_set_wait_budget", "laser_kv_paged_destroy",
 ]
 BF16, FP16 = range(2)
 
@@ -206,6 +206,8 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.laser_kv_paged_evict.argtypes = [vp, i32, i32, i32, vp]
     lib.laser_kv_paged_poll_status.restype = i32
     lib.laser_kv_paged_poll_status.argtypes = [vp, vp]
+    lib.laser_kv_paged_set_wait_budget.restype = i32
+    lib.laser_kv_paged_set_wait_budget.argtypes = [vp, C.c_uint32]
     lib.laser_kv_paged_destroy.restype = None
     lib.laser_kv_paged_destroy.argtypes = [vp]
     _pycall, _lib = _native_calls(lib, build_if_missing), lib
@@ -710,3 +712,6 @@ class PagedKV:
 
     def laser_kv_paged_poll_status(self, stream=None):
         _check(self.lib.laser_kv_paged_poll_status(self._h, _stream_ptr(stream)))
+
+    def laser_kv_paged_set_wait_budget(self, max_polls):
+        _check(self.lib.laser_kv_paged_set_wait_budget(self._h, max_polls))

@@ -67,13 +67,14 @@ struct PagedAttnArgs {
   float* scores;                                           // [tile of all heads][64][Gs]; NULL without weights
   float* weights;                                          // [n_pages][H][page_size]
   int2* score_at;                                          // [units of all heads] sequence and KV head of a tile of `scores`, tile of the sequence
-  int* score_units;                                        // units in use
+  int* score_units;                                        // units in use; behind it, nonzero: a wait of an attention ran out (8-byte aligned)
   int score_tiles;                                         // units that `scores` and `score_at` hold
   float* part;                                             // [2][grid] partials
   int* tickets;                                            // [n_seqs][H][head blocks] parts that are done; zero between calls
   int G, Gs, head_blocks;                                  // query heads per KV head, up to a power of two from 4 on; blocks of NG * 8 of them
   int out16;
   float scale_log2e;
+  uint32_t polls, poll_ns;                                 // budget of the waits for tiles, as of mbar_wait
 };
 
 template <int D>
@@ -269,6 +270,10 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const PagedPool& p = a.pool;
   const int heads = p.H * a.head_blocks;
+  auto give_up = [&]() {                                           // one thread: a wait ran out, the call's results are incomplete
+    record_status(p.status, kStatusTimeout);
+    if (a.scores) a.score_units[1] = 1;                            // no weight grows by them
+  };
 
   if (tid == kPagedWarps * 32) {
     for (int s = 0; s < kStages; ++s) { mbar_init(bar_full(s), 1); mbar_init(bar_empty(s), kPagedWarps); }
@@ -320,7 +325,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         const int rows = min(kDecTile, w.len - t * kDecTile), pages = (rows + (1 << rows_shift) - 1) >> rows_shift;
         const int id = __shfl_sync(0xffffffffu, ids, (k << per_shift) + (lane & ((1 << per_shift) - 1)));
         if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(bar_empty(st), (uint32_t)(round - 1) & 1u))) {
-          if (lane == 0) record_status(p.status, kStatusTimeout);
+          if (lane == 0) give_up();
           ok = false;                                              // the consumers' waits run out, too
           break;
         }
@@ -478,7 +483,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
   };
 
   int st = 0, round = 0;
-  bool gone = false;                                               // a wait ran out: the list is walked, nothing is computed
+  int gone = 0;                                                    // 1: a wait ran out, the list is walked, nothing is computed; 2: and no tile comes
   while (more) {
     const int t0 = w.first(begin), t1 = w.last(stop);
     if (t0 >= t1) break;                                           // the share ends with units of the item itself
@@ -489,10 +494,13 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         score_unit + tid < a.score_tiles)
       a.score_at[score_unit + tid] = make_int2(0, -1);               // units that are no tiles
     for (int t = t0; t < t1; ++t) {
-      if (!gone && !__all_sync(0xffffffffu, mbar_wait(bar_full(st), (uint32_t)round & 1u))) {
-        if (lane == 0) record_status(p.status, kStatusTimeout);
-        gone = true;
+      // Every warp waits for every tile, in order, also for one that it has no rows of and where it has given up: a wait tells
+      // rounds of a stage apart by their parity alone, and a stage that is freed before its tile has landed is filled twice at once.
+      if (!gone && !__all_sync(0xffffffffu, mbar_wait(bar_full(st), (uint32_t)round & 1u, a.polls, a.poll_ns))) {
+        if (lane == 0) give_up();
+        gone = 1;
       }
+      if (gone == 1 && !__all_sync(0xffffffffu, mbar_wait(bar_full(st), (uint32_t)round & 1u))) gone = 2;
       const int row0 = mate * (16 * NG), rows = w.len - t * kDecTile - row0;   // the warp's first row, how many the sequence has from there on
       if (!gone && rows > 0) {
         const uint32_t k_tile = base + st * paged_stage_bytes<D>(), v_tile = k_tile + kHalf;
@@ -591,7 +599,7 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         }
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(bar_empty(st));
+      if (lane == 0 && gone < 2) mbar_arrive(bar_empty(st));       // 2: the stage may yet be written, the producer gives up as well
       if (++st == kStages) { st = 0; ++round; }
     }
     // lanes with equal c hold different rows
@@ -669,19 +677,23 @@ paged_attn_kernel(const __grid_constant__ CUtensorMap map_k,      // keys: (D, p
         }
       };
       if (bulk) {
+        bool landed = true;
         for (int r = 0; r * kRound <= to - from; ++r) {
           const int n = min(kRound, to - from + 1 - r * kRound);
-          const bool landed = mbar_wait(bar_join(r & 1), (uint32_t)(r >> 1) & 1u);
-          if (!__all_sync(0xffffffffu, landed)) {
-            if (lane == 0) record_status(p.status, kStatusTimeout);
-          } else {
+          if (landed && !__all_sync(0xffffffffu, mbar_wait(bar_join(r & 1), (uint32_t)(r >> 1) & 1u))) {
+            landed = false;
+            if (lane == 0) give_up();
+            mbar_wait(bar_join(r & 1), (uint32_t)(r >> 1) & 1u);   // what is in flight, before the CTA ends
+            if ((r + 1) * kRound <= to - from) mbar_wait(bar_join((r + 1) & 1), (uint32_t)((r + 1) >> 1) & 1u);
+          }
+          if (landed) {
             for (int q = mate; q < n; q += kTeam) {
               const float4* src = reinterpret_cast<const float4*>(gen + (r & 1) * kRound * kPart * 4) + q * (kPart / 4);
               join(src[ml_at], [&](int mt) { return src[acc_at + mt * 32]; });
             }
           }
           paged_consumers_sync();                                  // the half is read
-          if (tid == 0) {
+          if (tid == 0 && landed) {
             fence_proxy_async_smem();
             fetch(r + 2);
           }
@@ -712,7 +724,8 @@ __global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(c
   const int quad = lane & (share - 1);                     // heads 4 quad .. 4 quad + 3
   grid_dependency_wait();
   allow_dependents();
-  const int total = *a.score_units;
+  const int2 units = *reinterpret_cast<const int2*>(a.score_units);
+  const int total = units.x;
   const int parts = a.score_tiles << share_shift;          // of a kilobyte each
   auto load = [&](int part, int2& at, float4 (&x)[2]) {    // behind the units in use lies what an earlier call left
     part = min(part, parts - 1);
@@ -725,13 +738,15 @@ __global__ void __launch_bounds__(256, kPagedWeightsCtas) paged_weights_kernel(c
   int2 at_next;
   float4 x_next[2];
   load(part, at_next, x_next);
-  const int n_parts = min(total, a.score_tiles) << share_shift;
+  // An attention that gave up leaves scores and normalisers of an earlier call, or of none: no weight grows until that is reported.
+  const int n_parts = units.y ? 0 : min(total, a.score_tiles) << share_shift;
+  const int most_tiles = ((p.max_pages << p.page_shift) + kDecTile - 1) / kDecTile;
   for (; part < n_parts; part += gridDim.x * 8) {
     const int2 at = at_next;
     const float4 x[2] = {x_next[0], x_next[1]};
     load(part + gridDim.x * 8, at_next, x_next);
     const int b = at.x & 0xFFFF, h = (int)((unsigned)at.x >> 16);
-    if (at.y < 0 || b >= p.n_seqs || h >= p.H) continue;   // a unit of an item itself, or the attention gave up
+    if ((unsigned)at.y >= (unsigned)most_tiles || b >= p.n_seqs || h >= p.H) continue;   // a unit of an item itself
     const float* z = a.lse2 + ((long long)b * p.H + h) * a.G;
     const int len = p.length(b), first = at.y * kDecTile + (((part & (share - 1)) * 64 + lane) >> share_shift);
     int page[2];

@@ -23,6 +23,7 @@ struct laser_kv_paged_ctx {
   long long n_moves = 0, cap = 0;
   int num_sms = 1;
   int evict_ctas = 1;                       // cluster of an eviction; 0: too many entries
+  uint32_t polls = 0;                       // 0: built-in wait budget (laser_kv_paged_set_wait_budget)
 };
 
 namespace {
@@ -71,7 +72,7 @@ laser_kv_status_t paged_derive(const laser_kv_paged_config_t* c, PagedDerived* d
     return fail(nullptr, LASER_KV_ERR_UNSUPPORTED, "paged config: weights for at most 128 query heads per KV head");
   size_t off = 0;
   auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes); return o; };
-  take(256);                                                   // status word, units of the last accumulating call
+  take(256);                                                   // status word; two words on, units of the last accumulating call and whether one gave up
   d->append_tickets = take((size_t)c->n_seqs * 4);
   d->attn_tickets = take((size_t)c->n_seqs * c->n_kv_heads * d->head_blocks * 4);
   d->zeroed = off;
@@ -345,12 +346,14 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
   a.G = h->group;
   a.Gs = h->score_heads;
   a.head_blocks = h->head_blocks;
+  a.polls = h->polls ? h->polls : kMaxPolls;
+  a.poll_ns = h->polls ? 0u : kPollHintNs;
   a.scale_log2e = (softmax_scale == 0.f ? 1.0f / std::sqrt((float)h->cfg.head_dim) : softmax_scale) * 1.4426950408889634f;
   if (accumulate) {
     a.lse2 = h->lse2;
     a.scores = h->scores;
     a.score_at = h->score_at;
-    a.score_units = reinterpret_cast<int*>(h->ws) + 1;
+    a.score_units = reinterpret_cast<int*>(h->ws) + 2;
     a.score_tiles = h->score_tiles;
     a.weights = h->rows.weights;
   }
@@ -410,6 +413,12 @@ laser_kv_status_t laser_kv_paged_poll_status(laser_kv_paged_handle_t h, void* st
     return fail(nullptr, LASER_KV_ERR_CAPACITY, "new entries did not fit their sequence's table, or sequences of a cache with weights share pages");
   if (word == kPagedBadPage) return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "a page number, a length or a count was out of range");
   if (word != 0) return fail(nullptr, (laser_kv_status_t)word, "device status word %d", word);
+  return LASER_KV_OK;
+}
+
+laser_kv_status_t laser_kv_paged_set_wait_budget(laser_kv_paged_handle_t h, uint32_t max_polls) {
+  if (!h) return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "paged_set_wait_budget: NULL handle");
+  h->polls = max_polls;
   return LASER_KV_OK;
 }
 
