@@ -486,7 +486,8 @@ laser_kv_status_t laser_kv_decode_attention(laser_kv_handle_t h, int32_t layer, 
  *                      strides will do (head by head or token by token within a page).
  *   weights          : dev fp32 [n_pages][n_kv_heads][page_size], the attention weight that an entry has received; NULL exactly
  *                      when config.track_weights is 0.
- *   pos              : dev int32 [n_pages][n_kv_heads][page_size], the entries' token positions.
+ *   pos              : dev int32 [n_pages][n_kv_heads][page_size], the entries' token positions; negative: not known, which protects
+ *                      an entry from no eviction. Appends write them; entries that the caller puts into the pool need the caller's.
  *   page_table       : dev int32 [n_seqs][max_pages]. Only the pages that hold a sequence's entries (and those that an append
  *                      fills) are looked up; the caller may change the table between calls. Pages that are appended to,
  *                      evicted from or that accumulate weights belong to one sequence alone; a cache without weights that is only read may share pages
@@ -564,7 +565,7 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
                                            float* lse, void* stream);
 
 /* Brings every sequence that holds more than `keep` entries back to `keep`, each KV head by itself: kept are the entries of positions
- * below `anchors`, those of the last `recent` positions seen (together at most `keep`; should positions repeat, so that more entries
+ * below `anchors`, those of positions from tokens seen - `recent` on (together at most `keep`; should positions repeat, so that more entries
  * than `keep` are among them, those of lowest index) and, up to `keep`, the ones of the largest accumulated weight; equal weights:
  * lower index first; NaN counts as -inf, +inf as protected. Entries stay where they are, except that the last kept entry behind `keep` moves
  * (key, value, weight, position) to the first slot before `keep` that an evicted one leaves, the last but one to the

@@ -589,7 +589,9 @@ class PagedKV:
     """One layer's paged cache over the caller's tensors: k_pages, v_pages [n_pages][H_kv][page_size][d] (bfloat16 or float16, or
     int16 for bfloat16's bits; any strides with a contiguous last dim), page_table int32 [n_seqs][max_pages], weights fp32 and pos
     int32 [n_pages][H_kv][page_size], state int32 [2][n_seqs] (entries held, tokens seen). pos and state are made here when not given;
-    without weights entries accumulate none and none can be evicted."""
+    without weights entries accumulate none and none can be evicted. In pos made here, where entries can be evicted, the slots of the
+    pages that page_table names have their places in the sequence as positions, but -1, not known, in sequences that have seen more
+    tokens than they hold."""
 
     def __init__(self, k_pages, v_pages, page_table, *, n_q_heads, weights=None, pos=None, state=None):
         import torch
@@ -600,7 +602,8 @@ class PagedKV:
         n_seqs, max_pages = page_table.shape
         dev = k_pages.device
         _need(k_pages.dtype in (torch.bfloat16, torch.float16, torch.int16), "paged cache: keys are bfloat16 or float16")
-        if pos is None:
+        own_pos = pos is None
+        if own_pos:
             pos = torch.full((n_pages, heads, page_size), -1, dtype=torch.int32, device=dev)
         if state is None:
             state = torch.zeros((2, n_seqs), dtype=torch.int32, device=dev)
@@ -616,6 +619,10 @@ class PagedKV:
                       f"paged cache: {name} must be a contiguous {dtype} tensor of shape {shape}")
         for t in (v_pages, page_table, pos, state, weights):
             _need(t is None or t.device == dev, "paged cache: tensors on different devices")
+        if own_pos and weights is not None:
+            known = (page_table >= 0) & (page_table < n_pages) & (state[0] == state[1])[:, None]
+            first = torch.arange(0, max_pages * page_size, page_size, dtype=torch.int32, device=dev).expand(n_seqs, -1)[known]
+            pos[page_table[known].long()] = first[:, None, None] + torch.arange(page_size, dtype=torch.int32, device=dev)
         self.k_pages, self.v_pages, self.page_table, self.weights, self.pos, self.state = k_pages, v_pages, page_table, weights, pos, state
         self.lens, self.seen = state[0], state[1]
         self.cfg = PagedConfig(n_seqs, n_q_heads, heads, d, page_size, n_pages, max_pages,

@@ -113,8 +113,8 @@ __global__ void __launch_bounds__(kPagedAppendThreads, kPagedAppendCtas) paged_a
 // ------------------------------------------------------------------------------------------------
 // Eviction. paged_evict_kernel: one cluster per (sequence, KV head); every CTA holds the sort keys of a slice of the entries in
 // shared memory.
-//   1. keys: the weight as an ordered integer, the largest for protected entries (the first positions and the last ones),
-//      -inf for NaN, which therefore leaves first.
+//   1. keys: the weight as an ordered integer, the largest for protected entries (the first positions and the last ones; a negative
+//      position is neither), -inf for NaN, which therefore leaves first.
 //   2. the keep-th largest key, by radix rounds over 11, 11 and 10 bits, the histograms summed across the cluster; protected
 //      keys, often the most, are counted apart, so that they do not pile up in one bin. (Starting from the smallest and the largest key, as
 //      take_topk does, takes one more barrier and gains nothing where some entries never received any weight.) A lone CTA ranks
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kEvictThreads, 1) paged_evict_kernel(const Pag
       if (i >= n) continue;
       const bool bad = (unsigned)page[j] >= (unsigned)p.n_pages;     // counts as -inf
       if (bad) record_status(p.status, kPagedBadPage);
-      const bool safe = !bad && (at[j] < a.anchors || at[j] >= newest || x[j] == INFINITY);
+      const bool safe = !bad && ((at[j] >= 0 && (at[j] < a.anchors || at[j] >= newest)) || x[j] == INFINITY);
       const uint32_t key = safe ? kEvictProtected : orderable_f32(bad || x[j] != x[j] ? -INFINITY : x[j] + 0.f);   // + 0: -0 is 0
       keys[i] = key;
       prot += safe;
