@@ -3,6 +3,7 @@ that run once per layer, block or token, by the native call path (csrc/pycall.cp
 owner of device memory and streams."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import importlib
 import os
@@ -275,6 +276,23 @@ def _stream_ptr(stream) -> int:
     return int(getattr(stream, "cuda_stream", stream))
 
 
+def _stream_object(stream, device):
+    """A torch stream for what a call's `stream` may be: one already, or a stream's handle."""
+    import torch
+    if hasattr(stream, "cuda_stream"):
+        return stream
+    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+
+
+def _allocating(stream, device):
+    """The context in which a call on `stream` takes memory: torch gives memory back to the stream that it was taken on, where work
+    queued earlier may still use it, and another stream does not wait for that."""
+    if stream is None:
+        return contextlib.nullcontext()
+    import torch
+    return torch.cuda.stream(_stream_object(stream, device))
+
+
 @dataclass
 class DebugTensors:
     s_exact: object
@@ -416,10 +434,15 @@ class LaserKV:
         scratch = self._decode_scratch
         if scratch is None:
             nbytes = int(self.lib.laser_kv_decode_attention_scratch_bytes(self.handle))
-            scratch = self._decode_scratch = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            self._decode_like = torch.empty(self._decode_shape, dtype=torch.float32, device=self.device)
+            with _allocating(stream, self.device):
+                scratch = self._decode_scratch = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+                self._decode_like = torch.empty(self._decode_shape, dtype=torch.float32, device=self.device)
         if out is None:
-            out = torch.empty_like(self._decode_like)            # 1.3 us less than from a shape
+            if stream is None:
+                out = torch.empty_like(self._decode_like)        # 1.3 us less than from a shape
+            else:
+                with _allocating(stream, self.device):
+                    out = torch.empty_like(self._decode_like)
         s = _pycall.decode_attention(self._h, layer, Q_dec.data_ptr(), qs, softmax_scale, out.data_ptr(), scratch.data_ptr(),
                                      scratch.numel(), _stream_ptr(stream))
         if s:
@@ -461,7 +484,8 @@ def laser_kv_two_stage_topk(s_exact, counts, anchors, k_exact, k_lsh, stream=Non
     import torch
     n_seg, S = s_exact.shape
     B = 2 * anchors + k_exact + k_lsh
-    idx = torch.empty((n_seg, B), dtype=torch.int32, device=s_exact.device)
+    with _allocating(stream, s_exact.device):
+        idx = torch.empty((n_seg, B), dtype=torch.int32, device=s_exact.device)
     load()
     _check(_pycall.two_stage_topk(_ptr(s_exact), _ptr(counts), n_seg, S, anchors, k_exact, k_lsh, _ptr(idx), _stream_ptr(stream)))
     return idx
@@ -491,9 +515,10 @@ def laser_kv_window_scores(K_blk, Q_win, block_size, n_blocks, softmax_scale=0.0
     batch, h_kv = K_blk.shape[0], K_blk.shape[1]
     h_q, window = Q_win.shape[1], Q_win.shape[2]
     need = laser_kv_window_scores_scratch_bytes(batch, h_q, h_kv, block_size, window, n_blocks)
-    if scratch is None:
-        scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=K_blk.device)
-    out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.float32, device=K_blk.device)
+    with _allocating(stream, K_blk.device):
+        if scratch is None:
+            scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=K_blk.device)
+        out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.float32, device=K_blk.device)
     _check(_pycall.window_scores(_ptr(K_blk), _ptr(Q_win), K_blk.stride(), Q_win.stride(), batch, h_q, h_kv, block_size, window,
                                  n_blocks, softmax_scale, _ptr(scratch), scratch.numel(), _ptr(out), _stream_ptr(stream)))
     return out
@@ -509,9 +534,10 @@ def laser_kv_collision_counts(K_blk, Q_win, hyperplanes, block_size, n_blocks, l
     h_q, window = Q_win.shape[1], Q_win.shape[2]
     need = int(load().laser_kv_collision_counts_scratch_bytes(batch, h_q, h_kv, block_size, window, n_blocks,
                                                               lsh_bits, lsh_tables))
-    if scratch is None:
-        scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=K_blk.device)
-    out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.int32, device=K_blk.device)
+    with _allocating(stream, K_blk.device):
+        if scratch is None:
+            scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=K_blk.device)
+        out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.int32, device=K_blk.device)
     _check(_pycall.collision_counts(_ptr(K_blk), _ptr(Q_win), _ptr(hyperplanes), K_blk.stride(), Q_win.stride(), batch, h_q, h_kv,
                                     block_size, window, n_blocks, lsh_bits, lsh_tables, _ptr(scratch), scratch.numel(),
                                     _ptr(out), _stream_ptr(stream)))
@@ -525,9 +551,10 @@ def laser_kv_collision_probability(K_blk, Q_win, block_size, n_blocks, lsh_bits,
     import torch
     batch, h_kv = K_blk.shape[0], K_blk.shape[1]
     h_q, window = Q_win.shape[1], Q_win.shape[2]
-    if scratch is None:
-        scratch = torch.empty(256, dtype=torch.uint8, device=K_blk.device)
-    out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.float32, device=K_blk.device)
+    with _allocating(stream, K_blk.device):
+        if scratch is None:
+            scratch = torch.empty(256, dtype=torch.uint8, device=K_blk.device)
+        out = torch.empty((batch, h_kv, n_blocks, block_size), dtype=torch.float32, device=K_blk.device)
     ks = (C.c_int64 * 3)(*K_blk.stride()[:3])
     qs = (C.c_int64 * 3)(*Q_win.stride()[:3])
     _check(load().laser_kv_collision_probability(_ptr(K_blk), _ptr(Q_win), ks, qs, batch, h_q, h_kv, block_size, window,
@@ -542,8 +569,9 @@ def laser_kv_consensus_accumulate(s_exact, counts, s_acc=None, c_acc=None, carry
     import torch
     batch, heads, nb, S = s_exact.shape
     if s_acc is None:
-        s_acc = torch.empty((batch, nb, S), dtype=torch.float32, device=s_exact.device)
-        c_acc = torch.empty((batch, nb, S), dtype=torch.int32, device=s_exact.device)
+        with _allocating(stream, s_exact.device):
+            s_acc = torch.empty((batch, nb, S), dtype=torch.float32, device=s_exact.device)
+            c_acc = torch.empty((batch, nb, S), dtype=torch.int32, device=s_exact.device)
     load()
     _check(_pycall.consensus_accumulate(_ptr(s_exact), _ptr(counts), batch, heads, nb, S, 1 if carry else 0, _ptr(s_acc),
                                         _ptr(c_acc), _stream_ptr(stream)))
@@ -591,7 +619,8 @@ class PagedKV:
     int32 [n_pages][H_kv][page_size], state int32 [2][n_seqs] (entries held, tokens seen). pos and state are made here when not given;
     without weights entries accumulate none and none can be evicted. In pos made here, where entries can be evicted, the slots of the
     pages that page_table names have their places in the sequence as positions, but -1, not known, in sequences that have seen more
-    tokens than they hold."""
+    tokens than they hold.
+    A call's stream is the current one or `stream`, a torch stream or a handle; results that a call allocates belong to it."""
 
     def __init__(self, k_pages, v_pages, page_table, *, n_q_heads, weights=None, pos=None, state=None):
         import torch
@@ -696,7 +725,11 @@ class PagedKV:
             self._refuse(Q, self._types, shape, "paged_attention: Q")
         is32 = 1
         if out is None:
-            out = self._empty(shape, dtype=f32, device=self._device)
+            if stream is None:
+                out = self._empty(shape, dtype=f32, device=self._device)
+            else:
+                with _allocating(stream, self._device):
+                    out = self._empty(shape, dtype=f32, device=self._device)
         else:
             is32 = out.dtype == f32
             if out.shape != shape or not out.is_contiguous() or not (is32 or out.dtype in self._types) or out.get_device() != dev:
