@@ -620,7 +620,9 @@ class PagedKV:
     without weights entries accumulate none and none can be evicted. In pos made here, where entries can be evicted, the slots of the
     pages that page_table names have their places in the sequence as positions, but -1, not known, in sequences that have seen more
     tokens than they hold.
-    A call's stream is the current one or `stream`, a torch stream or a handle; results that a call allocates belong to it."""
+    A call's stream is the current one or `stream`, a torch stream or a handle; results that a call allocates belong to it. Memory that is
+    made here is not given to others before the work that calls have queued is done, for which the streams of these calls have to be there
+    when the cache goes; a captured graph says nothing of its replays, so the cache has to outlive it."""
 
     def __init__(self, k_pages, v_pages, page_table, *, n_q_heads, weights=None, pos=None, state=None):
         import torch
@@ -631,10 +633,10 @@ class PagedKV:
         n_seqs, max_pages = page_table.shape
         dev = k_pages.device
         _need(k_pages.dtype in (torch.bfloat16, torch.float16, torch.int16), "paged cache: keys are bfloat16 or float16")
-        own_pos = pos is None
+        own_pos, own_state = pos is None, state is None
         if own_pos:
             pos = torch.full((n_pages, heads, page_size), -1, dtype=torch.int32, device=dev)
-        if state is None:
+        if own_state:
             state = torch.zeros((2, n_seqs), dtype=torch.int32, device=dev)
         _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.stride() == k_pages.stride(),
               "paged cache: v_pages differs from k_pages in shape, type or strides")
@@ -666,6 +668,8 @@ class PagedKV:
         self._device, self._index, self._f32, self._i32 = dev, dev.index, torch.float32, torch.int32
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)       # as _current_stream_getter, for the cache's device
         self._current = _stream_ptr if raw is None else lambda stream, index=dev.index: raw(index) if stream is None else _stream_ptr(stream)
+        self._home, self._others = self._current(None), set()              # the stream that owns the memory made here, others that use it
+        self._memory = [self.workspace] + [pos] * own_pos + [state] * own_state
         self._types = (torch.float16,) if k_pages.dtype == torch.float16 else (torch.bfloat16, torch.int16)
         self._q_shape, self._lse_shape = (n_seqs, n_q_heads, d), (n_seqs, n_q_heads)
         self._n_seqs, self._heads, self._d = n_seqs, heads, d
@@ -682,6 +686,14 @@ class PagedKV:
             self.close()
         except Exception:
             pass
+
+    def _used_on(self, stream):
+        """A call on a stream (its handle) that does not own the cache's memory: torch waits for it before it gives the memory away."""
+        if stream not in self._others:
+            s = _stream_object(stream, self._device)
+            for t in self._memory:
+                t.record_stream(s)
+            self._others.add(stream)
 
     def _refuse(self, t, dtypes, shape, name):
         raise LaserKVError(ERR_INVALID_ARG, f"{name}: expected {' or '.join(str(x) for x in dtypes)} {tuple(shape)} with a contiguous last "
@@ -713,7 +725,10 @@ class PagedKV:
             if pos.shape != (n_seqs, heads, n_new) or pos.dtype != i32 or pos.get_device() != dev or (n_new > 1 and ps[2] != 1):
                 self._refuse(pos, (i32,), (n_seqs, heads, n_new), "paged_append: pos")
             at = pos.data_ptr()
-        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, c, w, ws, at, ps, self._current(stream))
+        st = self._current(stream)
+        if st != self._home:
+            self._used_on(st)
+        s = _pycall.paged_append(self._h, K_new.data_ptr(), V_new.data_ptr(), ks, vs, n_new, c, w, ws, at, ps, st)
         if s:
             _check(s)
 
@@ -739,14 +754,19 @@ class PagedKV:
             if lse.shape != self._lse_shape or not lse.is_contiguous() or lse.dtype != f32 or lse.get_device() != dev:
                 self._refuse(lse, (f32,), self._lse_shape, "paged_attention: contiguous lse")
             z = lse.data_ptr()
-        s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(), is32, z,
-                                    self._current(stream))
+        st = self._current(stream)
+        if st != self._home:
+            self._used_on(st)
+        s = _pycall.paged_attention(self._h, Q.data_ptr(), qs, softmax_scale, 1 if accumulate else 0, out.data_ptr(), is32, z, st)
         if s:
             _check(s)
         return out
 
     def laser_kv_paged_evict(self, keep, anchors=0, recent=0, stream=None):
-        s = _pycall.paged_evict(self._h, keep, anchors, recent, self._current(stream))
+        st = self._current(stream)
+        if st != self._home:
+            self._used_on(st)
+        s = _pycall.paged_evict(self._h, keep, anchors, recent, st)
         if s:
             _check(s)
 
