@@ -496,6 +496,7 @@ laser_kv_status_t laser_kv_decode_attention(laser_kv_handle_t h, int32_t layer, 
  *                      that its next token gets. The calls below keep it; the caller may set it between calls (0 for a new
  *                      sequence, a smaller number of entries to take tokens back).
  *   workspace        : dev, 256-byte aligned, laser_kv_paged_query_sizes bytes, for this handle alone.
+ * Strides of a dimension of one entry are not looked at, here and in the calls below.
  * What unused slots hold is never interpreted (it may be NaN), and slots that no call is told to write keep it.
  * Lengths, counts and page numbers lie on the device, so the host does not see them: one out of range is not followed (nothing is
  * read or written outside the pool), recorded in the handle's status word, and the results of that sequence are

@@ -638,7 +638,8 @@ class PagedKV:
             pos = torch.full((n_pages, heads, page_size), -1, dtype=torch.int32, device=dev)
         if own_state:
             state = torch.zeros((2, n_seqs), dtype=torch.int32, device=dev)
-        _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and v_pages.stride() == k_pages.stride(),
+        steps = lambda t: [st for n, st in zip(t.shape, t.stride()) if n > 1]     # a dimension of one entry has no stride
+        _need(v_pages.shape == k_pages.shape and v_pages.dtype == k_pages.dtype and steps(v_pages) == steps(k_pages),
               "paged cache: v_pages differs from k_pages in shape, type or strides")
         _need(d == 1 or k_pages.stride(3) == 1, "paged cache: the last dimension must be contiguous")
         for name, t, dtype, shape in (("page_table", page_table, torch.int32, (n_seqs, max_pages)),

@@ -290,13 +290,16 @@ laser_kv_status_t laser_kv_paged_append(laser_kv_paged_handle_t h, const void* K
   if ((reinterpret_cast<uintptr_t>(counts) | reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(pos)) & 3u)
     return fail(nullptr, LASER_KV_ERR_ALIGNMENT, "paged_append: counts, weights and pos must be 4-byte aligned");
   PagedAppendArgs a{};
+  const int extents[3] = {h->cfg.n_seqs, h->cfg.n_kv_heads, n_new};
   for (int i = 0; i < 3; ++i) {
+    if (extents[i] == 1) continue;                                 // never stepped over
     if (k_strides[i] < 0 || v_strides[i] < 0 || (k_strides[i] % 8) || (v_strides[i] % 8))
       return fail(nullptr, LASER_KV_ERR_ALIGNMENT, "paged_append: strides must be non-negative multiples of 8 elements");
     a.ks[i] = k_strides[i];
     a.vs[i] = v_strides[i];
   }
   for (int i = 0; i < 2; ++i) {
+    if (extents[i] == 1) continue;
     a.ws[i] = weights ? w_strides[i] : 0;
     a.as[i] = pos ? pos_strides[i] : 0;
     if (a.ws[i] < 0 || a.as[i] < 0) return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "paged_append: negative stride");
@@ -327,7 +330,8 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
   if (!Q || !q_strides || !out) return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "paged_attention: NULL argument");
   if (!aligned16(Q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3u))
     return fail(nullptr, LASER_KV_ERR_ALIGNMENT, "paged_attention: Q and out must be 16-byte aligned, lse 4-byte aligned");
-  if (q_strides[0] < 0 || q_strides[1] < 0 || (q_strides[0] % 8) || (q_strides[1] % 8))
+  const int64_t qs_b = h->cfg.n_seqs == 1 ? 0 : q_strides[0], qs_h = h->cfg.n_q_heads == 1 ? 0 : q_strides[1];   // of one entry: never stepped over
+  if (qs_b < 0 || qs_h < 0 || (qs_b % 8) || (qs_h % 8))
     return fail(nullptr, LASER_KV_ERR_ALIGNMENT, "paged_attention: strides must be non-negative multiples of 8 elements");
   if (!(softmax_scale >= 0.f) || std::isinf(softmax_scale))
     return fail(nullptr, LASER_KV_ERR_INVALID_ARG, "paged_attention: softmax_scale must be positive (0 selects 1/sqrt(head_dim))");
@@ -336,8 +340,8 @@ laser_kv_status_t laser_kv_paged_attention(laser_kv_paged_handle_t h, const void
   PagedAttnArgs a{};
   a.pool = h->pool;
   a.Q = static_cast<const uint16_t*>(Q);
-  a.qs_b = q_strides[0];
-  a.qs_h = q_strides[1];
+  a.qs_b = qs_b;
+  a.qs_h = qs_h;
   a.out = out;
   a.out16 = out_fp32 ? 0 : 1;
   a.lse = lse;
