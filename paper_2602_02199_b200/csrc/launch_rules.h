@@ -130,7 +130,11 @@ LKV_HOST_DEVICE inline long long weighted_begin(long long part, int c, int n, co
 // (Divisions of 64 bits took a CTA 0.3 us to find its share.)
 // Where no item has more than kPagedWhole tiles, none is split: joining its parts would cost more than its tiles do one after the
 // other. Every item then counts kPagedWholeUnits units and the shares begin at items (`step`). us, split and whole: 8 items of 2
-// tiles 5.6 / 5.6, of 4 7.9 / 7.3, of 5 7.9 / 8.2, of 6 7.9 / 9.0; 512 items of 2 tiles 13.5 / 11.8.
+// tiles 5.6 / 5.6, of 4 7.9 / 7.3, of 5 7.9 / 8.2, of 6 7.9 / 9.0; 512 items of 2 tiles 13.5 / 11.8. Items of 4 tiles, 296 to 1000 of
+// them: 296 11.0 / 11.0, 304 16.3 / 15.2, 400 18.0 / 16.4, 600 23.3 / 22.2, 1000 30.3 / 29.3; of one tile alike. Of 10 to 256 entries, as they
+// come and with the short ones together: 296 12.7 / 8.7 and 12.9 / 8.4, 304 12.6 / 12.0 and 12.8 / 12.7, 400 12.7 / 13.2 and 12.8 / 13.3,
+// 600 15.4 / 16.3 and 15.7 / 17.6, 1000 19.8 / 23.0 and 19.8 / 23.6: whole items count alike, so many uneven ones are dealt unevenly, which costs
+// up to a sixth.
 constexpr int kPagedItemUnits = 2, kPagedWhole = 4, kPagedWholeUnits = kPagedWhole + kPagedItemUnits;
 struct PagedShares {
   int total, n, step, each, rest;          // units; shares of two units (or one item) at least; total / step = each * n + rest
@@ -154,9 +158,11 @@ struct PagedShares {
 
 // CTAs of the cluster that prunes one (sequence, KV head) of at most `cap` entries: kEvictOwn entries each while the device holds
 // all the call's clusters at once, at most kEvictKeys (their sort keys stay in shared memory). `room(n)`: how many clusters of n
-// the device holds at once, of sixteen seven on a B200. 0: more entries than the largest cluster holds. us for append and eviction of a block of
-// 4096 at a budget of 8192, 8 heads: clusters of one 39, of two 37, of four 31 (512 threads a CTA); at 32768 of eight 39, of
-// sixteen that take turns 62.
+// the device holds at once, of sixteen seven on a B200. 0: more entries than the largest cluster holds. us for append and eviction, by
+// clusters of one, two, four, eight: a block of 4096 at a budget of 8192, 8 heads 29.0, 27.9, 27.6, 28.7; of 8192 at 32768, 8 heads 67, 51, 45, 43,
+// of sixteen that take turns 64, and 32 heads 118, 102, 97, 126; a token at 4095, 32 heads 12.9, 15.4, 17.6, 43.5.
+// `cap` is the width of the table: lengths lie on the device. A table of more than kEvictKeys entries costs an eviction its
+// larger clusters whatever the sequences hold: 128 heads held at 2048, us at a table of 49152 11.2, 65536 26, 131072 55, 262144 125.
 constexpr int kEvictKeys = 49152, kEvictOwn = 4096;
 template <typename Room>
 inline int evict_cluster(long long heads, long long cap, Room&& room) {

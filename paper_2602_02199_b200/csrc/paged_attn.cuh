@@ -12,9 +12,10 @@
 //                         O^T += V^T P^T as m16n8k16 MMAs with the heads on the 8-wide side. A (sequence, head) that
 //                         crosses CTAs leaves partials; the CTA that finishes last joins them in a fixed order, so
 //                         results depend on lengths and shapes alone. 64 sequences of 4000 to 24000 entries, 8 heads of
-//                         four queries (2.94 GB): 435 us, 6.8 TB/s; one of 131,071 86.5 us, 6.2 TB/s. About 7 us are not
+//                         four queries (2.94 GB): 442 us, 6.6 TB/s; one of 131,071 87.2 us, 6.2 TB/s (a plain reduction over 2 GB reads at
+//                         6.85, a copy moves 6.52). About 7 us are not
 //                         streaming: the chain of length, page and first tile (3.5), merge, partial and join (3.5), each a
-//                         few trips to L2 of 0.5 to 0.9 us; small calls are made of them (1637 entries 9.4 us).
+//                         few trips to L2 of 0.5 to 0.9 us; small calls are made of them (1637 entries 9.6 us).
 //   paged_weights_kernel  exp(x_i - lse) from the scores that the first kernel left (4 bytes per query head and entry
 //                         against the 512 of its key and value), added to the entries' weights.
 //
