@@ -581,8 +581,8 @@ laser_kv_status_t laser_kv_paged_evict(laser_kv_paged_handle_t h, int32_t keep, 
 laser_kv_status_t laser_kv_paged_poll_status(laser_kv_paged_handle_t h, void* stream);
 
 /* Diagnostics, as laser_kv_set_wait_budget: poll budget of the attention's waits for tiles of keys and values (waits that free memory which a
- * copy may still write keep the built-in one). When it runs out, ERR_TIMEOUT is recorded, the results of that call are incomplete, and no weight
- * grows, by that call or a later one, until laser_kv_paged_poll_status has reported it. max_polls = 0: the built-in budget. Host only; applies
+ * copy may still write keep the built-in one). When it runs out, ERR_TIMEOUT is recorded and the results of that call are incomplete; if it
+ * accumulates, no weight grows, by that call or a later one, until laser_kv_paged_poll_status has reported it. max_polls = 0: the built-in budget. Host only; applies
  * to later calls on this handle. */
 laser_kv_status_t laser_kv_paged_set_wait_budget(laser_kv_paged_handle_t h, uint32_t max_polls);
 

@@ -279,9 +279,10 @@ def _stream_ptr(stream) -> int:
 def _stream_object(stream, device):
     """A torch stream for what a call's `stream` may be: one already, or a stream's handle."""
     import torch
-    if hasattr(stream, "cuda_stream"):
+    if isinstance(stream, torch.cuda.Stream):
         return stream
-    return torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+    handle = _stream_ptr(stream)
+    return torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
 
 
 def _allocating(stream, device):

@@ -40,6 +40,23 @@ def test_results_are_not_written_over_by_the_current_stream(raw):
         assert ((out.double() - want).abs() <= t_out).all()
 
 
+class Wrapped:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+def test_whatever_names_a_stream():
+    import numpy as np
+    cache, gen = build([300, 40], H=2, G=4, page_size=16)
+    q, side = queries(cache, gen), torch.cuda.Stream()
+    want = cache.laser_kv_paged_attention(q)
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream, np.int64(side.cuda_stream), Wrapped(side.cuda_stream), 0, torch.cuda.default_stream(), torch.cuda.ExternalStream(side.cuda_stream)):
+        out = cache.laser_kv_paged_attention(q, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+
+
 def test_results_of_the_compacted_cache_are_not_written_over():
     w = synth.workload("tiny").with_(block_size=512, context_len=2048, batch=2, n_layers=1, lsh_tables=16)
     run = run_workload_layer(w, 0, n_blocks=4, debug=0)
